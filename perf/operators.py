@@ -91,8 +91,8 @@ def draw(rng):
     nhi = rng.choice([1, 1, _log(rng, 2, 8), _log(rng, 9, 1024)])
     hi = _log(rng, 16, 16384)
     # At most half of the largest listed case's reads, and of the largest one's products.
-    at_most = min(400_000_000 // (heads["H"] * heads["d"] * hi),
-                  40_000_000_000 // (heads["H"] * G * heads["d"] * hi * nhi))
+    at_most = min(400_000_000 // (heads["H"] * heads["d"] * (hi + G * nhi)),
+                  40_000_000_000 // (heads["H"] * G * heads["d"] * (hi + nhi) * nhi))
     R = _log(rng, 1, max(1, min(256, at_most)))
     causal = rng.random() < 0.8
     return dict(heads, kind=kind, R=R, G=G, lo=rng.randint(0, hi), hi=hi,
