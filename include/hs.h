@@ -19,6 +19,10 @@
  *   hs_segment_sum           priority contribution of each fused node (Eq. 3)
  * and a batch's copies between host buffers and the device:
  *   hs_memcpy_async
+ * and the paged cache of keys and values that the merged model calls fill and read:
+ *   hs_kv_tables / hs_kv_release   block tables and slot maps from request lengths
+ *   hs_kv_append                   new keys and values, rounded to 8 bits
+ *   hs_kv_attend                   attention of new tokens' queries over the cache
  *
  * Conventions shared by every call
  *   - Pointers named *_dev or documented as device pointers must be device
@@ -599,6 +603,108 @@ hs_status hs_debug_retrieve_wait(uint64_t limit_ns, int32_t withhold_first);
 hs_status hs_debug_stream_rows(const int32_t* tokens, int64_t n_rows, int32_t row_stride,
                                const int32_t* lens, int32_t pattern, uint32_t* checksum_dev,
                                int32_t blocks_per_sm, hs_stream_t stream);
+
+/* ---- a paged cache of keys and values, 8 bits a value ---------------------------------
+ *
+ * Merged model calls run once, as requests of a batch.  Their keys and values
+ * live in blocks of block_tokens tokens:
+ *   k, v              codes [n_blocks, n_kv_heads, block_tokens, dim], contiguous
+ *   k_scale, v_scale  float [n_blocks, n_kv_heads]
+ * and a code c of block b and head h stands for c * scale[b, h].  A request's
+ * blocks are named by its row of a block table (int32 [n_req, table_width]):
+ * its token p is in block table[r, p / block_tokens] at offset
+ * p % block_tokens, and the slot of that token is
+ * block * block_tokens + offset.  Codes and scales of slots that no token was
+ * written to may hold anything.
+ *
+ * block_tokens: 16, 32, 64 or 128.  dim: 64, 128 or 256.  n_kv_heads >= 1.
+ * n_blocks * block_tokens <= 2^31 - 1.  The codes are 16-byte aligned.
+ */
+#define HS_KV_E4M3 0 /* codes are e4m3 values (4 bits of exponent, 3 of mantissa, no infinity) */
+#define HS_KV_INT8 1 /* codes are integers in [-127, 127]                                      */
+#define HS_KV_BF16 0 /* queries, new keys and values and outputs are bfloat16                  */
+#define HS_KV_FP16 1 /* ... IEEE half                                                          */
+
+/* Most requests of one hs_kv_* call. */
+#define HS_KV_MAX_REQUESTS 16384
+
+typedef struct {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int64_t n_blocks;
+  int32_t n_kv_heads;
+  int32_t block_tokens;
+  int32_t dim;
+  int32_t format; /* HS_KV_E4M3 or HS_KV_INT8 */
+} hs_kv_cache;
+
+/*
+ * hs_kv_tables — blocks and slots for the new tokens of a batch of requests.
+ *
+ * Request r has have[r] tokens in the cache and gets fresh[r] more.  Its new
+ * blocks are numbers ceil(have/bt) .. ceil((have+fresh)/bt) - 1 of its row of
+ * the table.  Free blocks wait in a ring: with cursor = {taken, given}, they
+ * are pool[taken % n_blocks], pool[(taken + 1) % n_blocks], ... up to number
+ * given - 1.  New blocks are taken in that order, by request and then by place.
+ *   table         device int32 [n_req, table_width], in place: entries of new
+ *                 blocks are written, all others are left as they are
+ *   starts_out    int32 [n_req + 1]: tokens of requests 0 .. r-1, so that the
+ *                 batch's token starts[r] + i is request r's i-th new one
+ *   lens_out      int32 [n_req]: have + fresh
+ *   slots_out     int32 [max_tokens]: the slot of each of the batch's tokens,
+ *                 -1 past their number
+ *   cursor_out    int64 [2]: {taken + new blocks, given}; not cursor itself
+ * n_req_dev (device int32 scalar, may be NULL) says how many of the n_req rows
+ * are requests; the others count as have = fresh = 0.
+ * Device errors (HS_ERR_INVALID_ARG in the error word): a negative length or
+ * more tokens than the table's row holds (the request then gets no tokens and
+ * lens 0); an entry of the table or of the pool that is no block (its tokens
+ * get slot -1); more than max_tokens tokens (the rest get no slot but keep
+ * their blocks); a ring that runs out (the requests that come last get slot -1
+ * and entry -1 past what is left, and their lens end with it).
+ */
+hs_status hs_kv_tables(const int32_t* have, const int32_t* fresh, int64_t n_req,
+                       const int32_t* n_req_dev, int32_t block_tokens, int32_t* table,
+                       int32_t table_width, const int32_t* pool, int64_t n_blocks,
+                       const int64_t* cursor, int64_t* cursor_out, int32_t* starts_out,
+                       int32_t* lens_out, int32_t* slots_out, int64_t max_tokens,
+                       hs_stream_t stream);
+
+/*
+ * hs_kv_release — the blocks of finished requests go back into the ring.
+ *
+ * lens[r] tokens of request r are given up (0: the request goes on): the
+ * first ceil(lens[r] / block_tokens) entries of its row of the table are
+ * appended to the ring, cursor_out = {taken, given + their number}.  Entries
+ * that are no block, lengths that the row does not hold and blocks that the
+ * ring has no room for set the device error word and are left out.
+ */
+hs_status hs_kv_release(const int32_t* lens, int64_t n_req, const int32_t* n_req_dev,
+                        int32_t block_tokens, const int32_t* table, int32_t table_width,
+                        int32_t* pool, int64_t n_blocks, const int64_t* cursor,
+                        int64_t* cursor_out, hs_stream_t stream);
+
+/*
+ * hs_kv_append — the batch's new keys and values into their slots.
+ *
+ * k, v: device [n_tokens, n_kv_heads, dim] of `dtype` (HS_KV_BF16 or
+ * HS_KV_FP16); token_stride and head_stride are in elements, a head's dim
+ * values are contiguous.  slots: int32 [n_tokens], -1 for a token that is not
+ * written.  Tokens of one block stand next to each other in the batch, in the
+ * order of their slots, as hs_kv_tables lays them out (a block named in two
+ * places of the batch is written by both, in no order).
+ * A block's scale is the least power of two, not below 2^-126, with
+ * |x| <= 448 * scale (e4m3) or 127 * scale (int8) over the new tokens' finite
+ * values; a block that has tokens before its first new one keeps the larger of
+ * that and its own, and where its scale grows their codes are rounded to the
+ * new one.  Rounding is to nearest even; infinities saturate; a NaN is NaN in
+ * e4m3 and 0 in int8.  Slots without a new token are left alone but for that.
+ */
+hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, int32_t dtype,
+                       int64_t n_tokens, int64_t token_stride, int64_t head_stride,
+                       const int32_t* slots, hs_stream_t stream);
 
 #ifdef __cplusplus
 }

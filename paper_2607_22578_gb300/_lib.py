@@ -26,6 +26,11 @@ HS_ERR_TIMEOUT = 5
 HS_FNV64_OFFSET_BASIS = 0xCBF29CE484222325
 HS_TOPK_MAX_K = 1024
 HS_MERGE_QUERIES_MAX = 256
+HS_KV_E4M3 = 0
+HS_KV_INT8 = 1
+HS_KV_BF16 = 0
+HS_KV_FP16 = 1
+HS_KV_MAX_REQUESTS = 16384
 
 _STATUS = {0: "HS_OK", 1: "HS_ERR_INVALID_ARG", 2: "HS_ERR_UNSUPPORTED", 3: "HS_ERR_CUDA",
            4: "HS_ERR_WORKSPACE", 5: "HS_ERR_TIMEOUT"}
@@ -113,6 +118,12 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
             lib.hs_memcpy_async.restype = st
             lib.hs_debug_stream_rows.argtypes = [P, i64, i32, P, i32, P, i32, P]
             lib.hs_debug_stream_rows.restype = st
+            lib.hs_kv_tables.argtypes = [P, P, i64, P, i32, P, i32, P, i64, P, P, P, P, P, i64, P]
+            lib.hs_kv_tables.restype = st
+            lib.hs_kv_release.argtypes = [P, i64, P, i32, P, i32, P, i64, P, P, P]
+            lib.hs_kv_release.restype = st
+            lib.hs_kv_append.argtypes = [P, P, P, i32, i64, i64, i64, P, P]
+            lib.hs_kv_append.restype = st
             _lib = lib
     return _lib
 
@@ -566,6 +577,146 @@ def hs_segment_sum(phi: torch.Tensor, inverse: torch.Tensor, max_groups: int,
     _check(load().hs_segment_sum(_ptr(phi), _ptr(inverse), phi.numel(), _ptr(n_groups_dev),
                                  int(max_groups), _ptr(out), _stream(stream)))
     return _rows(out, int(max_groups))
+
+
+class _KvCacheStruct(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("n_blocks", ctypes.c_int64),
+                ("n_kv_heads", ctypes.c_int32), ("block_tokens", ctypes.c_int32),
+                ("dim", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+_KV_CODES = {torch.float8_e4m3fn: HS_KV_E4M3, torch.int8: HS_KV_INT8}
+_KV_DTYPES = {torch.bfloat16: HS_KV_BF16, torch.float16: HS_KV_FP16}
+
+
+class KvCache:
+    """Paged cache of keys and values, 8 bits a value: codes ``k`` and ``v``
+    [n_blocks, n_kv_heads, block_tokens, dim] (torch.float8_e4m3fn or
+    torch.int8) and float32 scales [n_blocks, n_kv_heads]; a code stands for
+    itself times its block and head's scale.  Allocated here, or ``of``
+    tensors that a program has."""
+
+    def __init__(self, n_blocks: int, block_tokens: int, n_kv_heads: int, dim: int,
+                 dtype: torch.dtype = torch.float8_e4m3fn, device=None):
+        if dtype not in _KV_CODES:
+            raise TypeError("a cache holds torch.float8_e4m3fn or torch.int8")
+        shape = (int(n_blocks), int(n_kv_heads), int(block_tokens), int(dim))
+        dev = device or "cuda"
+        self._take(*(torch.empty(shape, dtype=dtype, device=dev) for _ in range(2)),
+                   *(torch.zeros(shape[:2], dtype=torch.float32, device=dev) for _ in range(2)))
+
+    @classmethod
+    def of(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor,
+           v_scale: torch.Tensor) -> "KvCache":
+        self = cls.__new__(cls)
+        self._take(k, v, k_scale, v_scale)
+        return self
+
+    def _take(self, k, v, k_scale, v_scale):
+        for t, name in ((k, "k"), (v, "v"), (k_scale, "k_scale"), (v_scale, "v_scale")):
+            _cuda(t, name)
+        if k.dtype not in _KV_CODES or v.dtype != k.dtype:
+            raise TypeError("k and v must both be torch.float8_e4m3fn or torch.int8")
+        if k.dim() != 4 or v.shape != k.shape:
+            raise ValueError("k and v must be [n_blocks, n_kv_heads, block_tokens, dim]")
+        for t in (k_scale, v_scale):
+            if t.dtype != torch.float32 or t.shape != k.shape[:2]:
+                raise TypeError("scales must be float32 [n_blocks, n_kv_heads]")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_blocks, self.n_kv_heads, self.block_tokens, self.dim = k.shape
+        self._struct = _KvCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(),
+                                      v_scale.data_ptr(), *k.shape, _KV_CODES[k.dtype])
+        self._at = ctypes.addressof(self._struct)
+
+
+def _i32(t, name: str, n: int | None = None):
+    """t as a contiguous int32 CUDA tensor of n elements."""
+    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous int32 CUDA tensor" % name)
+    if n is not None and t.numel() != n:
+        raise ValueError("%s must have %d elements" % (name, n))
+    return t.data_ptr()
+
+
+def _kv_cursor(t, name: str):
+    if t.dtype != torch.int64 or not t.is_cuda or t.numel() != 2 or not t.is_contiguous():
+        raise TypeError("%s must be a contiguous int64 CUDA tensor of 2 elements" % name)
+    return t.data_ptr()
+
+
+def hs_kv_tables(have: torch.Tensor, fresh: torch.Tensor, table: torch.Tensor, pool: torch.Tensor,
+                 cursor: torch.Tensor, block_tokens: int, max_tokens: int,
+                 n_req_dev: torch.Tensor | None = None, out: tuple | None = None, stream=None):
+    """Blocks and slots for the ``fresh[r]`` new tokens of requests that have
+    ``have[r]`` in the cache.  ``table`` [n_req, width] gets the new blocks,
+    taken from the ring ``pool`` [n_blocks] at ``cursor`` = {taken, given}
+    (int64 [2]).  Returns (slots [max_tokens], starts [n_req + 1], lens
+    [n_req], cursor [2]), or writes them to ``out``; max_tokens is the number
+    of new tokens, or more (slot -1 past them)."""
+    n = have.numel()
+    if table.dim() != 2 or table.shape[0] != n:
+        raise ValueError("table must be [n_req, width]")
+    max_tokens = int(max_tokens)
+    if out is None:
+        new = have.new_empty
+        out = (new(max_tokens), new(n + 1), new(n), cursor.new_empty(2))
+    slots, starts, lens, after = out
+    _check(load().hs_kv_tables(
+        _i32(have, "have"), _i32(fresh, "fresh", n), n,
+        None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"), int(block_tokens),
+        _i32(table, "table"), table.shape[1], _i32(pool, "pool"), pool.numel(),
+        _kv_cursor(cursor, "cursor"), _kv_cursor(after, "cursor out"),
+        _i32(starts, "starts", n + 1), _i32(lens, "lens", n), _i32(slots, "slots", max_tokens),
+        max_tokens, _stream(stream)))
+    return slots, starts, lens, after
+
+
+def hs_kv_release(lens: torch.Tensor, table: torch.Tensor, pool: torch.Tensor,
+                  cursor: torch.Tensor, block_tokens: int,
+                  n_req_dev: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                  stream=None) -> torch.Tensor:
+    """The blocks of ``lens[r]`` tokens of each finished request (0: it goes
+    on) go back into the ring.  Returns the cursor after that."""
+    n = lens.numel()
+    if table.dim() != 2 or table.shape[0] != n:
+        raise ValueError("table must be [n_req, width]")
+    if out is None:
+        out = cursor.new_empty(2)
+    _check(load().hs_kv_release(
+        _i32(lens, "lens"), n, None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"),
+        int(block_tokens), _i32(table, "table"), table.shape[1], _i32(pool, "pool"),
+        pool.numel(), _kv_cursor(cursor, "cursor"), _kv_cursor(out, "cursor out"),
+        _stream(stream)))
+    return out
+
+
+def _kv_heads(t, name: str, dim: int):
+    """t's data pointer and dtype code: a CUDA tensor [tokens, heads, dim] of
+    bf16 or fp16 values whose heads are contiguous."""
+    dtype = _KV_DTYPES.get(t.dtype)
+    if dtype is None or not t.is_cuda:
+        raise TypeError("%s must be a CUDA tensor of bfloat16 or float16" % name)
+    if t.dim() != 3 or t.shape[2] != dim or t.stride(2) != 1:
+        raise ValueError("%s must be [tokens, heads, dim] with contiguous heads of the cache's dim"
+                         % name)
+    return t.data_ptr(), dtype
+
+
+def hs_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
+                 stream=None) -> None:
+    """Write new keys and values [tokens, n_kv_heads, dim] (views with strides
+    of their own, the same for both, are fine) into their slots, rounded to
+    the cache's codes; block scales grow as they have to."""
+    kp, dtype = _kv_heads(k, "k", cache.dim)
+    vp, vtype = _kv_heads(v, "v", cache.dim)
+    T, H, _ = k.shape
+    if v.shape != k.shape or H != cache.n_kv_heads or vtype != dtype:
+        raise ValueError("k and v must both be [tokens, n_kv_heads, dim] of one dtype")
+    if v.stride() != k.stride():
+        raise ValueError("k and v must have the same strides")
+    _check(load().hs_kv_append(cache._at, kp, vp, dtype, T, k.stride(0), k.stride(1),
+                               _i32(slots, "slots", T), _stream(stream)))
 
 
 def hs_launch_count() -> int:

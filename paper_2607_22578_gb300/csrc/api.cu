@@ -41,6 +41,13 @@ hs_status launch_merge_queries(const uint16_t*, int64_t, int32_t, uint64_t, cons
                                uint64_t*, int32_t*, int32_t*, int32_t*, uint16_t*, cudaStream_t);
 hs_status launch_scatter(const void*, int64_t, int64_t, const int32_t*, int64_t, void*,
                          cudaStream_t);
+hs_status launch_kv_tables(const int32_t*, const int32_t*, int64_t, const int32_t*, int32_t,
+                           int32_t*, int32_t, const int32_t*, int64_t, const int64_t*, int64_t*,
+                           int32_t*, int32_t*, int32_t*, int64_t, cudaStream_t);
+hs_status launch_kv_release(const int32_t*, int64_t, const int32_t*, int32_t, const int32_t*,
+                            int32_t, int32_t*, int64_t, const int64_t*, int64_t*, cudaStream_t);
+hs_status launch_kv_append(const hs_kv_cache&, int32_t, const uint16_t*, const uint16_t*, int32_t,
+                           int64_t, int64_t, int64_t, const int32_t*, cudaStream_t);
 
 namespace {
 thread_local char g_msg[512] = "";
@@ -476,6 +483,117 @@ hs_status hs_memcpy_async(void* dst, const void* src, size_t bytes, hs_stream_t 
   return cuda_fail(cudaMemcpyAsync(dst, src, bytes, cudaMemcpyDefault,
                                    reinterpret_cast<cudaStream_t>(stream)),
                    "copy");
+}
+
+// ---- the paged cache of keys and values ----------------------------------------------------
+
+// log2 of a block's tokens, or -1 if the library has no kernel for that many.
+static int block_log2(int32_t bt) {
+  return bt == 16 ? 4 : bt == 32 ? 5 : bt == 64 ? 6 : bt == 128 ? 7 : -1;
+}
+
+static hs_status check_requests(int64_t n_req, const int32_t* n_req_dev) {
+  if (n_req < 0) return fail(HS_ERR_INVALID_ARG, "n_req < 0");
+  if (n_req > HS_KV_MAX_REQUESTS)
+    return fail(HS_ERR_UNSUPPORTED, "n_req > %d", HS_KV_MAX_REQUESTS);
+  if (n_req_dev && !aligned(n_req_dev, 4))
+    return fail(HS_ERR_INVALID_ARG, "n_req_dev misaligned");
+  return HS_OK;
+}
+
+static hs_status check_blocks(int32_t block_tokens, int64_t n_blocks, int32_t width) {
+  if (block_log2(block_tokens) < 0)
+    return fail(HS_ERR_UNSUPPORTED, "block_tokens must be 16, 32, 64 or 128");
+  if (n_blocks < 1 || n_blocks * block_tokens > 0x7fffffffLL || n_blocks > 0x7fffffffLL)
+    return fail(HS_ERR_INVALID_ARG, "n_blocks < 1 or n_blocks * block_tokens > 2^31 - 1");
+  if (width < 1 || (int64_t)width * block_tokens > 0x7fffffffLL)
+    return fail(HS_ERR_INVALID_ARG, "table_width < 1 or table_width * block_tokens > 2^31 - 1");
+  return HS_OK;
+}
+
+static hs_status check_cache(const hs_kv_cache* c) {
+  if (!c) return fail(HS_ERR_INVALID_ARG, "cache is NULL");
+  if (const hs_status st = check_blocks(c->block_tokens, c->n_blocks, 1)) return st;
+  if (c->dim != 64 && c->dim != 128 && c->dim != 256)
+    return fail(HS_ERR_UNSUPPORTED, "dim must be 64, 128 or 256");
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 65535)
+    return fail(HS_ERR_INVALID_ARG, "n_kv_heads outside [1, 65535]");
+  if (c->format != HS_KV_E4M3 && c->format != HS_KV_INT8)
+    return fail(HS_ERR_INVALID_ARG, "format is neither HS_KV_E4M3 nor HS_KV_INT8");
+  if (!c->k || !c->v || !c->k_scale || !c->v_scale)
+    return fail(HS_ERR_INVALID_ARG, "NULL pointer in the cache");
+  if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->k_scale, 4) ||
+      !aligned(c->v_scale, 4))
+    return fail(HS_ERR_INVALID_ARG, "misaligned pointer in the cache (codes 16 B, scales 4 B)");
+  return HS_OK;
+}
+
+hs_status hs_kv_tables(const int32_t* have, const int32_t* fresh, int64_t n_req,
+                       const int32_t* n_req_dev, int32_t block_tokens, int32_t* table,
+                       int32_t table_width, const int32_t* pool, int64_t n_blocks,
+                       const int64_t* cursor, int64_t* cursor_out, int32_t* starts_out,
+                       int32_t* lens_out, int32_t* slots_out, int64_t max_tokens,
+                       hs_stream_t stream) {
+  clear_msg();
+  if (const hs_status st = check_requests(n_req, n_req_dev)) return st;
+  if (const hs_status st = check_blocks(block_tokens, n_blocks, table_width)) return st;
+  if (max_tokens < 0 || max_tokens > 0x7fffffffLL)
+    return fail(HS_ERR_INVALID_ARG, "max_tokens outside [0, 2^31 - 1]");
+  if (!cursor || !cursor_out || !starts_out || !pool)
+    return fail(HS_ERR_INVALID_ARG, "NULL cursor, cursor_out, starts_out or pool");
+  if (cursor == cursor_out) return fail(HS_ERR_INVALID_ARG, "cursor_out is cursor");
+  if (n_req > 0 && (!have || !fresh || !table || !lens_out))
+    return fail(HS_ERR_INVALID_ARG, "NULL have, fresh, table or lens_out");
+  if (max_tokens > 0 && !slots_out) return fail(HS_ERR_INVALID_ARG, "slots_out is NULL");
+  if (!aligned(have, 4) || !aligned(fresh, 4) || !aligned(table, 4) || !aligned(pool, 4) ||
+      !aligned(cursor, 8) || !aligned(cursor_out, 8) || !aligned(starts_out, 4) ||
+      !aligned(lens_out, 4) || !aligned(slots_out, 4))
+    return fail(HS_ERR_INVALID_ARG, "misaligned pointer (cursors 8 B, others 4 B)");
+  return launch_kv_tables(have, fresh, n_req, n_req_dev, block_log2(block_tokens), table,
+                          table_width, pool, n_blocks, cursor, cursor_out, starts_out, lens_out,
+                          slots_out, max_tokens, reinterpret_cast<cudaStream_t>(stream));
+}
+
+hs_status hs_kv_release(const int32_t* lens, int64_t n_req, const int32_t* n_req_dev,
+                        int32_t block_tokens, const int32_t* table, int32_t table_width,
+                        int32_t* pool, int64_t n_blocks, const int64_t* cursor,
+                        int64_t* cursor_out, hs_stream_t stream) {
+  clear_msg();
+  if (const hs_status st = check_requests(n_req, n_req_dev)) return st;
+  if (const hs_status st = check_blocks(block_tokens, n_blocks, table_width)) return st;
+  if (!cursor || !cursor_out || !pool)
+    return fail(HS_ERR_INVALID_ARG, "NULL cursor, cursor_out or pool");
+  if (cursor == cursor_out) return fail(HS_ERR_INVALID_ARG, "cursor_out is cursor");
+  if (n_req > 0 && (!lens || !table)) return fail(HS_ERR_INVALID_ARG, "NULL lens or table");
+  if (!aligned(lens, 4) || !aligned(table, 4) || !aligned(pool, 4) || !aligned(cursor, 8) ||
+      !aligned(cursor_out, 8))
+    return fail(HS_ERR_INVALID_ARG, "misaligned pointer (cursors 8 B, others 4 B)");
+  return launch_kv_release(lens, n_req, n_req_dev, block_log2(block_tokens), table, table_width,
+                           pool, n_blocks, cursor, cursor_out,
+                           reinterpret_cast<cudaStream_t>(stream));
+}
+
+static hs_status check_dtype(int32_t dtype) {
+  if (dtype != HS_KV_BF16 && dtype != HS_KV_FP16)
+    return fail(HS_ERR_INVALID_ARG, "dtype is neither HS_KV_BF16 nor HS_KV_FP16");
+  return HS_OK;
+}
+
+hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, int32_t dtype,
+                       int64_t n_tokens, int64_t token_stride, int64_t head_stride,
+                       const int32_t* slots, hs_stream_t stream) {
+  clear_msg();
+  if (const hs_status st = check_cache(cache)) return st;
+  if (const hs_status st = check_dtype(dtype)) return st;
+  if (n_tokens < 0 || n_tokens > 0x7fffffffLL)
+    return fail(HS_ERR_INVALID_ARG, "n_tokens outside [0, 2^31 - 1]");
+  if (n_tokens == 0) return HS_OK;
+  if (!k || !v || !slots) return fail(HS_ERR_INVALID_ARG, "NULL k, v or slots");
+  if (!aligned(k, 2) || !aligned(v, 2) || !aligned(slots, 4))
+    return fail(HS_ERR_INVALID_ARG, "misaligned pointer (k, v 2 B, slots 4 B)");
+  return launch_kv_append(*cache, block_log2(cache->block_tokens), static_cast<const uint16_t*>(k),
+                          static_cast<const uint16_t*>(v), dtype, n_tokens, token_stride,
+                          head_stride, slots, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"
