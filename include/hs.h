@@ -706,6 +706,42 @@ hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, i
                        int64_t n_tokens, int64_t token_stride, int64_t head_stride,
                        const int32_t* slots, hs_stream_t stream);
 
+/*
+ * hs_kv_attend — attention of the batch's queries over the cache.
+ *
+ * Request r has lens[r] = L tokens in the cache and n = starts[r + 1] -
+ * starts[r] queries, the batch's tokens starts[r] .. (starts NULL: max_q
+ * each).  Its query i stands at position L - n + i; head h of n_heads reads
+ * kv head h / (n_heads / n_kv_heads).  Over the keys j < L that it sees (all;
+ * causal: j <= L - n + i, and with window > 0 also j > L - n + i - window),
+ *   lse = log sum_j exp(scale * q . k_j)
+ *   out = sum_j exp(scale * q . k_j - lse) v_j
+ * A query that sees no key gets zeros and lse = -inf.  causal = 0 is cross
+ * attention: an encoder's L states under n queries of another length.
+ *
+ * q           [n_tokens, n_heads, dim] of dtype; strides in elements, a head's
+ *             values contiguous (16-byte aligned rows take wide loads).
+ * max_q       the most queries of a request.
+ * table       int32 [n_req, table_width]; the entries of L tokens are read.
+ * out         [n_tokens, n_heads, dim] of dtype, contiguous.
+ * lse         float [n_tokens, n_heads], or NULL.
+ * workspace   hs_kv_attend_workspace() bytes, 256-byte aligned, zeroed once
+ *             before its first use; every call leaves it fit for the next.
+ * Products of 16-bit values with fp32 sums; q, k and v are exact in them, the
+ * weights are rounded to half.  Results do not depend on the order in which
+ * the kernel's blocks finish.
+ * Device errors (HS_ERR_INVALID_ARG in the error word): starts or lens that
+ * cannot be (the request's rows are left as they were), a table entry that is
+ * no block (its tokens count as zeros).
+ */
+size_t hs_kv_attend_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t dim, int32_t max_q);
+hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, int64_t n_tokens,
+                       int32_t n_heads, int64_t token_stride, int64_t head_stride,
+                       const int32_t* lens, const int32_t* starts, int64_t n_req,
+                       const int32_t* n_req_dev, int32_t max_q, const int32_t* table,
+                       int32_t table_width, float scale, int32_t causal, int32_t window, void* out,
+                       float* lse, void* workspace, size_t workspace_bytes, hs_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

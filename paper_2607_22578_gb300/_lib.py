@@ -124,6 +124,11 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
             lib.hs_kv_release.restype = st
             lib.hs_kv_append.argtypes = [P, P, P, i32, i64, i64, i64, P, P]
             lib.hs_kv_append.restype = st
+            lib.hs_kv_attend_workspace.argtypes = [i32, i32, i32, i32]
+            lib.hs_kv_attend_workspace.restype = sz
+            lib.hs_kv_attend.argtypes = [P, P, i32, i64, i32, i64, i64, P, P, i64, P, i32, P, i32,
+                                         ctypes.c_float, i32, i32, P, P, P, sz, P]
+            lib.hs_kv_attend.restype = st
             _lib = lib
     return _lib
 
@@ -717,6 +722,58 @@ def hs_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
         raise ValueError("k and v must have the same strides")
     _check(load().hs_kv_append(cache._at, kp, vp, dtype, T, k.stride(0), k.stride(1),
                                _i32(slots, "slots", T), _stream(stream)))
+
+
+def hs_kv_attend_workspace(cache: KvCache, n_heads: int, max_q: int) -> int:
+    """Bytes of hs_kv_attend's workspace, which is zeroed once."""
+    return int(load().hs_kv_attend_workspace(int(n_heads), cache.n_kv_heads, cache.dim, int(max_q)))
+
+
+def hs_kv_attend(cache: KvCache, q: torch.Tensor, lens: torch.Tensor, table: torch.Tensor,
+                 starts: torch.Tensor | None = None, max_q: int | None = None,
+                 scale: float | None = None, causal: bool = True, window: int = 0,
+                 n_req_dev: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                 out: tuple | None = None, stream=None):
+    """Attention of queries q [tokens, n_heads, dim] over the cache.  Request
+    r has lens[r] tokens there, in the blocks of row r of ``table``, and the
+    queries starts[r] .. starts[r + 1] - 1, at its last positions; without
+    ``starts`` every request has tokens / n_req of them.  ``max_q`` is the
+    most queries of a request (all of them, if it is not given).  Returns
+    (out, shaped and typed like q, and lse float32 [tokens, n_heads])."""
+    qp, dtype = _kv_heads(q, "q", cache.dim)
+    T, heads, dim = q.shape
+    n = lens.numel()
+    if table.dim() != 2 or table.shape[0] != n:
+        raise ValueError("table must be [n_req, width]")
+    if starts is None:
+        if n and T % n:
+            raise ValueError("without starts, every request has as many queries")
+        each = T // n if n else 0
+        if max_q is not None and int(max_q) != each:
+            raise ValueError("max_q is not what every request has")
+        max_q = each
+    elif max_q is None:
+        max_q = T
+    if out is None:
+        out = (torch.empty((T, heads, dim), dtype=q.dtype, device=q.device),
+               torch.empty((T, heads), dtype=torch.float32, device=q.device))
+    o, lse = out
+    if o.dtype != q.dtype or o.shape != q.shape or not o.is_cuda or not o.is_contiguous():
+        raise ValueError("out must be contiguous and like q")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2]
+                            or not lse.is_cuda or not lse.is_contiguous()):
+        raise ValueError("lse must be contiguous float32 [tokens, n_heads]")
+    if workspace is None:
+        workspace = torch.zeros(hs_kv_attend_workspace(cache, heads, max_q), dtype=torch.uint8,
+                                device=q.device)
+    _check(load().hs_kv_attend(
+        cache._at, qp, dtype, T, heads, q.stride(0), q.stride(1), _i32(lens, "lens"),
+        None if starts is None else _i32(starts, "starts", n + 1), n,
+        None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"), int(max_q),
+        _i32(table, "table"), table.shape[1], dim ** -0.5 if scale is None else scale,
+        int(causal), int(window), o.data_ptr(), None if lse is None else lse.data_ptr(),
+        workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    return o, lse
 
 
 def hs_launch_count() -> int:

@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "hs_internal.cuh"
+#include "kv_attend.cuh"
 
 namespace hs {
 
@@ -48,6 +49,8 @@ hs_status launch_kv_release(const int32_t*, int64_t, const int32_t*, int32_t, co
                             int32_t, int32_t*, int64_t, const int64_t*, int64_t*, cudaStream_t);
 hs_status launch_kv_append(const hs_kv_cache&, int32_t, const uint16_t*, const uint16_t*, int32_t,
                            int64_t, int64_t, int64_t, const int32_t*, cudaStream_t);
+size_t attend_workspace(int32_t);
+hs_status launch_kv_attend(AttendParams, int32_t, int32_t, int64_t, void*, cudaStream_t);
 
 namespace {
 thread_local char g_msg[512] = "";
@@ -594,6 +597,76 @@ hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, i
   return launch_kv_append(*cache, block_log2(cache->block_tokens), static_cast<const uint16_t*>(k),
                           static_cast<const uint16_t*>(v), dtype, n_tokens, token_stride,
                           head_stride, slots, reinterpret_cast<cudaStream_t>(stream));
+}
+
+size_t hs_kv_attend_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t dim, int32_t max_q) {
+  if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || max_q < 0) return 0;
+  if (dim != 64 && dim != 128 && dim != 256) return 0;
+  return attend_workspace(dim);
+}
+
+hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, int64_t n_tokens,
+                       int32_t n_heads, int64_t token_stride, int64_t head_stride,
+                       const int32_t* lens, const int32_t* starts, int64_t n_req,
+                       const int32_t* n_req_dev, int32_t max_q, const int32_t* table,
+                       int32_t table_width, float scale, int32_t causal, int32_t window, void* out,
+                       float* lse, void* workspace, size_t workspace_bytes, hs_stream_t stream) {
+  clear_msg();
+  if (const hs_status st = check_cache(cache)) return st;
+  if (const hs_status st = check_dtype(dtype)) return st;
+  if (const hs_status st = check_requests(n_req, n_req_dev)) return st;
+  if (n_heads < 1 || n_heads % cache->n_kv_heads)
+    return fail(HS_ERR_INVALID_ARG, "n_heads is no multiple of n_kv_heads");
+  if (n_tokens < 0 || max_q < 0 || n_tokens * n_heads > 0x7fffffffLL ||
+      (int64_t)max_q * n_heads > 0x3fffffffLL)
+    return fail(HS_ERR_INVALID_ARG, "n_tokens * n_heads or max_q * n_heads out of range");
+  if (!starts && (int64_t)max_q * n_req > n_tokens)
+    return fail(HS_ERR_INVALID_ARG, "no starts, and n_req * max_q > n_tokens");
+  if (table_width < 1 || (int64_t)table_width * cache->block_tokens > 0x7fffff00LL)
+    return fail(HS_ERR_INVALID_ARG, "table_width < 1 or table_width * block_tokens > 2^31 - 256");
+  if (window < 0) return fail(HS_ERR_INVALID_ARG, "window < 0");
+  if (window > 0 && !causal) return fail(HS_ERR_INVALID_ARG, "a window needs causal");
+  if (!(scale > 0.0f) || scale > 3.0e38f) return fail(HS_ERR_INVALID_ARG, "scale must be positive");
+  if (n_req == 0 || n_tokens == 0 || max_q == 0) return HS_OK;
+  if (!q || !lens || !table || !out) return fail(HS_ERR_INVALID_ARG, "NULL q, lens, table or out");
+  if (!aligned(q, 2) || !aligned(out, 16) || !aligned(lens, 4) || !aligned(starts, 4) ||
+      !aligned(table, 4) || !aligned(lse, 4))
+    return fail(HS_ERR_INVALID_ARG, "misaligned pointer (q 2 B, out 16 B, others 4 B)");
+  const size_t need = attend_workspace(cache->dim);
+  if (!workspace || !aligned(workspace, 256))
+    return fail(HS_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned");
+  if (workspace_bytes < need)
+    return fail(HS_ERR_WORKSPACE, "attend workspace too small: %zu < %zu", workspace_bytes, need);
+  AttendParams p{};
+  p.k = static_cast<const uint8_t*>(cache->k);
+  p.v = static_cast<const uint8_t*>(cache->v);
+  p.ks = cache->k_scale;
+  p.vs = cache->v_scale;
+  p.n_blocks = (int32_t)cache->n_blocks;
+  p.H = cache->n_kv_heads;
+  p.G = n_heads / cache->n_kv_heads;
+  p.bt_log2 = block_log2(cache->block_tokens);
+  p.q = static_cast<const uint16_t*>(q);
+  p.q_token = token_stride;
+  p.q_head = head_stride;
+  p.q_vec = token_stride % 8 == 0 && head_stride % 8 == 0 && aligned(q, 16);
+  p.fp16 = dtype == HS_KV_FP16;
+  p.n_tokens = (int32_t)n_tokens;
+  p.max_q = max_q;
+  p.lens = lens;
+  p.starts = starts;
+  p.n_req = (int32_t)n_req;
+  p.n_req_dev = n_req_dev;
+  p.table = table;
+  p.width = table_width;
+  p.causal = causal != 0;
+  // a window that holds every token hides none
+  p.window = (int64_t)window >= (int64_t)table_width * cache->block_tokens ? 0 : window;
+  p.scale_log2 = scale * 1.4426950408889634f;
+  p.out = static_cast<uint16_t*>(out);
+  p.lse = lse;
+  return launch_kv_attend(p, cache->dim, cache->format, (int64_t)max_q * p.G, workspace,
+                          reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

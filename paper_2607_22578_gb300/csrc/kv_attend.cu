@@ -1,0 +1,756 @@
+// Attention of few query rows over the paged 8-bit cache (hs_kv_attend): single tokens, drafts,
+// and every other length by groups of rows.
+//
+// For a request with L tokens in the cache and n queries, query i sits at position L - n + i, and
+//   s_ij = scale * q_i . k_j,  o_i = sum_j exp(s_ij - lse_i) v_j,  lse_i = log sum_j exp(s_ij)
+// over the keys j < L that it sees.  The keys and values of a kv head are shared by the G query
+// heads of its group, so the rows of a tile are (query, head of the group): 8 * NT of them.
+//
+// Reading the codes once is all the work there is (2 * dim bytes a token against 2 * G flops a
+// byte), so the kernel is built around keeping loads in flight:
+//  - The work is cut into units of 128 tokens of one (request, kv head, group of rows), laid end
+//    to end, and every CTA takes an equal share of the list, whatever the lengths are.  Where a
+//    (request, head, group) is cut between CTAs, each leaves its partial result in the workspace
+//    and the one that comes last merges them in their order: no second launch, and a result that
+//    does not depend on which was last.
+//  - A warp takes 32 of a unit's tokens through a ring of its own in shared memory (cp.async,
+//    codes and scales, tokens past the end as zeros, so what stale slots hold is never read) and
+//    keeps its own running maximum and sum: no barrier until a (request, head, group) ends.
+//  - Products are on mma.sync m16n8k16 with tokens as M and rows as N: a decoding step has 1 to 16
+//    rows, which would fill an eighth of a tcgen05 tile's 128, and codes go straight from shared
+//    memory to registers as half2 (exact for e4m3 and int8).
+// Arithmetic: q as half after division by a power of two of its row (exact but below 2^-24 of the
+// row's largest), products and sums in fp32, p = 2^(s - m + 7) as half (the running maximum m may
+// lag by 8, so p <= 2^15; what is under 2^-31 of the largest is dropped from o, not from lse),
+// scales of value blocks relative to the largest so far, divided out at the end.
+#include "kv_cache.cuh"
+#include "kv_attend.cuh"
+
+namespace hs {
+namespace {
+
+constexpr int kAttWarps = 4;
+constexpr int kAttThreads = kAttWarps * 32;
+constexpr int kWarpTokens = 32;                          // of a unit, for each warp
+constexpr int kUnitTokens = kAttWarps * kWarpTokens;
+constexpr int kAttStages = 2;
+constexpr float kLag = 8.0f;                             // of the running maximum, in powers of two
+constexpr float kShift = 7.0f;
+
+template <int D>
+constexpr int stage_bytes() { return 2 * kWarpTokens * D + 16; }  // K, V, two scales of each
+
+// Where 16-byte chunk c of token row r of a tile lies, so that both ways of reading it (8 tokens
+// by 2 chunks, 4 even tokens by 2 chunks) touch every bank once.
+template <int D>
+__device__ __forceinline__ uint32_t chunk_at(int r, int c) {
+  if constexpr (D == 64)
+    return (uint32_t)((r >> 1) * 128 + (((r ^ (r >> 2)) & 1) << 6) + ((c ^ (r & 2)) << 4));
+  else
+    return (uint32_t)(r * D + (c & ~7) * 16 + (((c ^ r) & 7) << 4));
+}
+
+__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+               "r"(in ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src),
+               "r"(in ? 4 : 0)
+               : "memory");
+}
+
+__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                          uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+  return v;
+}
+
+// A place in the list of units: a (request, kv head, group of rows) and one of its tiles.
+struct Place {
+  int32_t r, h, group, groups;
+  int32_t tile, tile0, tile_end;   // tiles of kUnitTokens tokens
+  int32_t n, q0, len;
+};
+
+struct Request {
+  int32_t n, q0, len, groups, tile0, tiles;
+};
+
+// What request r asks for; groups = 0 if nothing (or nothing that can be done: *bad).
+__device__ __forceinline__ Request request(const AttendParams& p, int32_t r, int32_t rows,
+                                           unsigned* bad) {
+  Request q;
+  q.groups = 0;
+  q.tile0 = 0;
+  q.tiles = 0;
+  if (!attend_request(p, r, q.n, q.q0, q.len, bad)) return q;
+  if (q.n * p.G > p.rows_most) return q;                // another kernel's
+  q.groups = (q.n * p.G + rows - 1) / rows;
+  if (p.window > 0) {
+    const int32_t first = q.len - q.n - p.window + 1;
+    if (first > 0) q.tile0 = first / kUnitTokens;
+  }
+  q.tiles = max((q.len + kUnitTokens - 1) / kUnitTokens - q.tile0, 1);  // an empty one too
+  return q;
+}
+
+template <int D, int NT, int FMT>
+__global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendParams p) {
+  constexpr int ROWS = 8 * NT;
+  constexpr int HALVES = D == 64 ? 1 : D / 128;  // 128-byte pieces of a row (D = 64: one of 64)
+  constexpr int KS = D == 64 ? 4 : 8;            // k16 steps, and m16 tiles of dim, of a piece
+  constexpr int NO = HALVES * KS * NT * 4;       // output registers of a thread
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ int64_t sums[kAttWarps];
+  __shared__ int64_t found_units;
+  __shared__ int32_t found_r, last_s;
+  __shared__ float m_s[kAttWarps][ROWS];
+
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int g = lane >> 2, c = lane & 3;
+  uint8_t* ring = smem + warp * (kAttStages * stage_bytes<D>());
+  float* merge = reinterpret_cast<float*>(smem + kAttWarps * kAttStages * stage_bytes<D>());
+  const uint32_t ring_u = smem_u32(ring);
+
+  pdl_wait();
+  pdl_trigger();
+  const int32_t R = p.n_req_dev ? max(0, min(__ldg(p.n_req_dev), p.n_req)) : p.n_req;
+
+  // ---- how many units there are, and which are this CTA's
+  unsigned bad = 0;
+  const int32_t per = (R + kAttThreads - 1) / kAttThreads;
+  const int32_t ra = min(tid * per, R), rb = min(ra + per, R);
+  int64_t mine = 0;
+  for (int32_t r = ra; r < rb; ++r) {
+    const Request q = request(p, r, ROWS, &bad);
+    mine += (int64_t)q.groups * q.tiles;
+  }
+  mine *= p.H;
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31) sums[warp] = incl;
+  __syncthreads();
+  int64_t U = 0, before = 0;
+#pragma unroll
+  for (int w = 0; w < kAttWarps; ++w) {
+    if (w == warp) before = U;
+    U += sums[w];
+  }
+  const int64_t E = min((int64_t)gridDim.x, U);           // CTAs with work
+  if (bad && blockIdx.x == 0) set_error(p.err, bad);
+  if (blockIdx.x >= E) return;
+  const int64_t u_begin = U * blockIdx.x / E, u_end = U * (blockIdx.x + 1) / E;
+  before += incl - mine;
+  if (u_begin >= before && u_begin < before + mine) {     // one thread's requests hold the first
+    int64_t at = before;
+    int32_t r = ra;
+    for (; r + 1 < rb; ++r) {
+      const Request q = request(p, r, ROWS, &bad);
+      const int64_t n = (int64_t)q.groups * q.tiles * p.H;
+      if (u_begin < at + n) break;
+      at += n;
+    }
+    found_r = r;
+    found_units = u_begin - at;
+  }
+  __syncthreads();
+
+  Place fetch;                                            // what is loaded next
+  const auto open = [&](Place& w, int32_t r, int64_t skip) {
+    Request q{0, 0, 0, 1, 0, 1};                          // (of none, should the lengths change)
+    for (; r < R; ++r) {
+      const Request x = request(p, r, ROWS, &bad);
+      if (x.groups > 0) {
+        q = x;
+        break;
+      }
+    }
+    w.r = r;
+    w.groups = q.groups;
+    w.n = q.n;
+    w.q0 = q.q0;
+    w.len = q.len;
+    w.tile0 = q.tile0;
+    w.tile_end = q.tile0 + q.tiles;
+    w.h = (int32_t)(skip / ((int64_t)q.groups * q.tiles));
+    skip -= (int64_t)w.h * q.groups * q.tiles;
+    w.group = (int32_t)(skip / q.tiles);
+    w.tile = q.tile0 + (int32_t)(skip - (int64_t)w.group * q.tiles);
+  };
+  const auto step = [&](Place& w) {                       // to the next unit of the list
+    if (++w.tile < w.tile_end) return;
+    w.tile = w.tile0;
+    if (++w.group < w.groups) return;
+    w.group = 0;
+    if (++w.h < p.H) return;
+    open(w, w.r + 1, 0);
+  };
+  open(fetch, found_r, found_units);
+
+  // ---- loading: this warp's 32 tokens of a unit, one stage
+  const int two = p.bt_log2 == 4;                         // its tokens lie in two blocks
+  int32_t id0 = 0, id1 = 0;
+  const auto look_up = [&]() {                            // the blocks of `fetch`
+    const int32_t t0 = fetch.tile * kUnitTokens + warp * kWarpTokens;
+    const int32_t* row = p.table + (int64_t)fetch.r * p.width + (t0 >> p.bt_log2);
+    id0 = t0 < fetch.len ? __ldg(row) : 0;
+    id1 = two && t0 + 16 < fetch.len ? __ldg(row + 1) : id0;
+  };
+  const auto load = [&](int stage) {
+    const int32_t t0 = fetch.tile * kUnitTokens + warp * kWarpTokens;
+    int32_t left = fetch.len - t0;                        // tokens that there are
+    if ((uint32_t)id0 >= (uint32_t)p.n_blocks || (uint32_t)id1 >= (uint32_t)p.n_blocks) {
+      if (left > 0) set_error(p.err, kErrInvalidArg);
+      left = 0;
+    }
+    const uint32_t base = ring_u + stage * stage_bytes<D>();
+    if (left > 0) {
+      const int64_t in = (int64_t)(t0 & ((1 << p.bt_log2) - 1)) * D;
+      const int64_t b0 = ((((int64_t)id0 * p.H + fetch.h) << p.bt_log2) * D) + in;
+      const int64_t b1 = two ? (((int64_t)id1 * p.H + fetch.h) << 4) * D - 16 * D : b0;
+      constexpr int CH = D / 16;                          // chunks of a row
+#pragma unroll
+      for (int i = 0; i < kWarpTokens * CH / 32; ++i) {
+        const int at = i * 32 + lane, r = at / CH, ch = at % CH;
+        const int64_t off = (r < 16 ? b0 : b1) + r * D + ch * 16;
+        const bool ok = r < left;
+        const uint32_t dst = base + chunk_at<D>(r, ch);
+        cp_async16_zfill(dst, p.k + (ok ? off : 0), ok);
+        cp_async16_zfill(dst + kWarpTokens * D, p.v + (ok ? off : 0), ok);
+      }
+      if (lane < 4) {
+        const float* s = lane < 2 ? p.ks : p.vs;
+        const bool ok = (lane & 1) * 16 < left;
+        const int64_t at = (int64_t)((lane & 1) ? id1 : id0) * p.H + fetch.h;
+        cp_async4_zfill(base + 2 * kWarpTokens * D + lane * 4, s + (ok ? at : 0), ok);
+      }
+    } else {
+      for (int at = lane * 16; at < stage_bytes<D>(); at += 512)
+        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + at), "r"(0)
+                     : "memory");
+    }
+  };
+
+  const int64_t units = u_end - u_begin;
+  int64_t fetched = 0;
+  look_up();
+  Place at = fetch;                                       // what is computed next
+#pragma unroll
+  for (int s = 0; s < kAttStages - 1; ++s) {
+    if (fetched < units) {
+      load(s);
+      if (++fetched < units) {
+        step(fetch);
+        look_up();
+      }
+    }
+    cp_async_commit();
+  }
+
+  uint32_t qf[HALVES][KS][NT][2];
+  float o[HALVES][KS][NT][4];
+  float mx[NT][2], sum[NT][2], qs[NT][2];
+  int32_t top[NT][2], bottom[NT][2];                      // keys that a row sees: bottom .. top
+  float v_ref = 0.0f;
+  int stage = 0;
+  bool fresh = true;
+  int32_t seg_tile = 0;                                   // the first tile that this CTA has of it
+
+  for (int64_t u = 0; u < units; ++u) {
+    if (fresh) {                                          // a (request, head, group) begins
+      fresh = false;
+      seg_tile = at.tile;
+      v_ref = 1.17549435e-38f;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int row = at.group * ROWS + nt * 8 + g;
+        const bool in = row < at.n * p.G;
+        const int i = in ? row / p.G : 0, j = in ? row - i * p.G : 0;
+        const uint16_t* q = p.q + (int64_t)(at.q0 + i) * p.q_token + (int64_t)(at.h * p.G + j) * p.q_head;
+        float x[HALVES][KS][4];
+        float big = 0.0f;
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf) {
+          const uint16_t* src = q + hf * 128 + c * (KS * 4);
+#pragma unroll
+          for (int k = 0; k < KS; k += 2) {
+            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            if (in) attend_load8(src + k * 4, p.q_vec, p.fp16, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              x[hf][k + (e >> 2)][e & 3] = f[e];
+              big = fmaxf(big, fabsf(f[e]));
+            }
+          }
+        }
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        // a power of two of the row's size, kept where it and its inverse are normal
+        const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+        const float by = __uint_as_float((254u - e) << 23);
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            qf[hf][k][nt][0] = pack_half2(x[hf][k][0] * by, x[hf][k][1] * by);
+            qf[hf][k][nt][1] = pack_half2(x[hf][k][2] * by, x[hf][k][3] * by);
+          }
+        const float back = __uint_as_float(e << 23) * p.scale_log2;
+#pragma unroll
+        for (int e2 = 0; e2 < 2; ++e2) {
+          qs[nt][e2] = __shfl_sync(0xffffffffu, back, (2 * c + e2) * 4);
+          mx[nt][e2] = -INFINITY;
+          sum[nt][e2] = 0.0f;
+          const int row2 = at.group * ROWS + nt * 8 + 2 * c + e2;
+          const int pos = at.len - at.n + row2 / p.G;
+          top[nt][e2] = p.causal ? min(pos, at.len - 1) : at.len - 1;
+          bottom[nt][e2] = p.window > 0 ? pos - p.window + 1 : 0;
+        }
+      }
+#pragma unroll
+      for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[hf][k][nt][e] = 0.0f;
+    }
+
+    cp_async_wait<kAttStages - 2>();
+    __syncwarp();
+    {  // the next load goes where the last unit was
+      const int s = stage == 0 ? kAttStages - 1 : stage - 1;
+      if (fetched < units) {
+        load(s);
+        if (++fetched < units) {
+          step(fetch);
+          look_up();
+        }
+      }
+      cp_async_commit();
+    }
+    const uint32_t kb = ring_u + stage * stage_bytes<D>(), vb = kb + kWarpTokens * D;
+    float scales[4];
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(scales[0]), "=f"(scales[1]), "=f"(scales[2]), "=f"(scales[3])
+                 : "r"(kb + 2 * kWarpTokens * D)
+                 : "memory");
+    const int32_t t0 = at.tile * kUnitTokens + warp * kWarpTokens;
+    if (t0 < at.len) {
+      // ---- s = q . k: tokens are M, rows are N
+      float s[2][NT][4];
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.0f;
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf) {
+          uint32_t a[2][KS];
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int r = mt * 16 + x * 8 + g;
+#pragma unroll
+            for (int k = 0; k < KS; k += 4) {
+              const uint4 w = lds128(kb + chunk_at<D>(r, hf * 8 + (KS / 4) * c + k / 4));
+              a[x][k] = w.x;
+              a[x][k + 1] = w.y;
+              a[x][k + 2] = w.z;
+              a[x][k + 3] = w.w;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const uint32_t a0 = KvFormat<FMT>::template decode2<0>(a[0][k]);
+            const uint32_t a1 = KvFormat<FMT>::template decode2<0>(a[1][k]);
+            const uint32_t a2 = KvFormat<FMT>::template decode2<1>(a[0][k]);
+            const uint32_t a3 = KvFormat<FMT>::template decode2<1>(a[1][k]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              mma_16816(s[mt][nt], a0, a1, a2, a3, qf[hf][k][nt][0], qf[hf][k][nt][1]);
+          }
+        }
+      }
+      // ---- masks, running maximum
+      const bool whole = t0 + kWarpTokens <= (p.causal ? at.len - at.n + 1 : at.len) &&
+                         (p.window <= 0 || t0 > at.len - 1 - p.window);
+      float most[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float m = -INFINITY;
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float& z = s[mt][nt][2 * x + e];
+              z *= scales[mt] * qs[nt][e];
+              if (!whole) {
+                const int t = t0 + mt * 16 + x * 8 + g;
+                if (t > top[nt][e] || t < bottom[nt][e]) z = -INFINITY;
+              }
+              m = fmaxf(m, z);
+            }
+          most[nt][e] = m;
+        }
+      bool grow = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) grow |= most[nt][e] > mx[nt][e] + kLag;
+      const float v_top = fmaxf(v_ref, fmaxf(scales[2], scales[3]));
+      const bool v_grow = v_top > v_ref;
+      if (__any_sync(0xffffffffu, grow || v_grow)) {
+        const float vr = v_grow ? __fdividef(v_ref, v_top) : 1.0f;
+        v_ref = v_top;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float m = most[nt][e];
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+            m = fmaxf(m, mx[nt][e]);
+            const float f = m == -INFINITY ? 1.0f : exp2f(mx[nt][e] - m);
+            mx[nt][e] = m;
+            sum[nt][e] *= f;
+#pragma unroll
+            for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+              for (int k = 0; k < KS; ++k) {
+                o[hf][k][nt][e] *= f * vr;
+                o[hf][k][nt][2 + e] *= f * vr;
+              }
+          }
+      }
+      // ---- p = 2^(s - m + 7), and o += p . v with dim as M, rows as N, tokens as K
+      const float inv_ref = __fdividef(1.0f, v_ref);
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        const float ratio = scales[2 + mt] * inv_ref;
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float m = mx[nt][e] == -INFINITY ? 0.0f : mx[nt][e] - kShift;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              float& z = s[mt][nt][2 * x + e];
+              z = exp2f(z - m);
+              sum[nt][e] += z;
+              z *= ratio;
+            }
+          }
+          pb[nt][0] = transpose_8x8(pack_half2(s[mt][nt][0], s[mt][nt][1]));
+          pb[nt][1] = transpose_8x8(pack_half2(s[mt][nt][2], s[mt][nt][3]));
+        }
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf) {
+          uint32_t w[4][KS / 2];                          // tokens 2c, 2c+1, 2c+8, 2c+9
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int r = mt * 16 + 2 * c + (x & 1) + (x >> 1) * 8;
+            if constexpr (D == 64) {
+              const uint2 y = lds64(vb + chunk_at<D>(r, g >> 1) + (g & 1) * 8);
+              w[x][0] = y.x;
+              w[x][1] = y.y;
+            } else {
+              const uint4 y = lds128(vb + chunk_at<D>(r, hf * 8 + g));
+              w[x][0] = y.x;
+              w[x][1] = y.y;
+              w[x][2] = y.z;
+              w[x][3] = y.w;
+            }
+          }
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            const uint32_t sel = (k & 1) ? 0x7362u : 0x5140u;
+            const uint32_t lo = __byte_perm(w[0][k / 2], w[1][k / 2], sel);
+            const uint32_t hi = __byte_perm(w[2][k / 2], w[3][k / 2], sel);
+            const uint32_t a0 = KvFormat<FMT>::template decode2<0>(lo);
+            const uint32_t a1 = KvFormat<FMT>::template decode2<1>(lo);
+            const uint32_t a2 = KvFormat<FMT>::template decode2<0>(hi);
+            const uint32_t a3 = KvFormat<FMT>::template decode2<1>(hi);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              mma_16816(o[hf][k][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+          }
+        }
+      }
+    }
+    if (++stage == kAttStages) stage = 0;
+    const bool ends = at.tile + 1 == at.tile_end;
+    if (!ends && u + 1 < units) {
+      ++at.tile;
+      continue;
+    }
+
+    // ---- the CTA's part of this (request, head, group) is done: its warps' results together
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1)
+          sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], x);
+        if (g == 0) m_s[warp][nt * 8 + 2 * c + e] = mx[nt][e];
+      }
+    __syncthreads();
+    float big[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kAttWarps; ++w) m = fmaxf(m, m_s[w][nt * 8 + 2 * c + e]);
+        big[nt][e] = m;
+        const float f = mx[nt][e] == -INFINITY ? 0.0f : exp2f(mx[nt][e] - m);
+        sum[nt][e] *= f;
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            o[hf][k][nt][e] *= f * v_ref;
+            o[hf][k][nt][2 + e] *= f * v_ref;
+          }
+      }
+#pragma unroll
+    for (int half = kAttWarps / 2; half > 0; half >>= 1) {
+      float* mine_s = merge + (warp % half) * (NO + 2 * NT) * 32 + lane;
+      if (warp >= half && warp < 2 * half) {
+#pragma unroll
+        for (int i = 0; i < NO; ++i) mine_s[i * 32] = (&o[0][0][0][0])[i];
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) mine_s[(NO + i) * 32] = (&sum[0][0])[i];
+      }
+      __syncthreads();
+      if (warp < half) {
+#pragma unroll
+        for (int i = 0; i < NO; ++i) (&o[0][0][0][0])[i] += mine_s[i * 32];
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) (&sum[0][0])[i] += mine_s[(NO + i) * 32];
+      }
+      __syncthreads();
+    }
+    const bool all_of_it = seg_tile == at.tile0 && ends;
+    // Output of rows by threads that hold values of dim 16 g + 2 k + {0, 1} (D = 64: 8 g + ...)
+    const auto write = [&](int k0, int k1) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = at.group * ROWS + nt * 8 + 2 * c + e;
+          if (row >= at.n * p.G) continue;
+          const int i = row / p.G, j = row - i * p.G;
+          const int64_t r = (int64_t)(at.q0 + i) * (p.H * p.G) + at.h * p.G + j;
+          const float l = sum[nt][e];
+          const float inv = l > 0.0f ? __fdividef(1.0f, l) : (l == 0.0f ? 0.0f : l);
+#pragma unroll
+          for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+              if (k >= k0 && k < k1)
+                attend_store2(p.out + r * D + hf * 128 + g * (2 * KS) + 2 * k, p.fp16,
+                              o[hf][k][nt][e] * inv, o[hf][k][nt][2 + e] * inv);
+          if (g == 0 && k0 == 0 && p.lse)
+            p.lse[r] = l == 0.0f ? -INFINITY
+                                 : (big[nt][e] - kShift + log2f(l)) * 0.69314718055994531f;
+        }
+    };
+    if (all_of_it) {
+      if (warp == 0) write(0, KS);
+    } else {
+      // Partial results: the part that begins at this CTA's first unit in its slot 0, one that
+      // begins later (and so runs past its last) in slot 1.
+      const int64_t first = u_begin + u - (at.tile - at.tile0);       // units of the whole
+      const int64_t last = first + (at.tile_end - at.tile0) - 1;
+      const int32_t c0 = (int32_t)(((first + 1) * E - 1) / U), c1 = (int32_t)(((last + 1) * E - 1) / U);
+      constexpr int PS = (NO + 4 * NT) * 32;
+      const auto slot_of = [&](int32_t cta) {
+        return p.partial + ((int64_t)cta * 2 + (cta == c0 && first > U * cta / E ? 1 : 0)) * PS + lane;
+      };
+      if (warp == 0) {
+        float* d = slot_of(blockIdx.x);
+#pragma unroll
+        for (int i = 0; i < NO; ++i) __stcg(d + i * 32, (&o[0][0][0][0])[i]);
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) {
+          __stcg(d + (NO + i) * 32, (&big[0][0])[i]);
+          __stcg(d + (NO + 2 * NT + i) * 32, (&sum[0][0])[i]);
+        }
+        __threadfence();
+        __syncwarp();
+        if (lane == 0) last_s = atomicAdd(p.counters + c0, 1u) == (unsigned)(c1 - c0);
+      }
+      __syncthreads();
+      if (last_s) {                                       // everyone else has left its part
+        __threadfence();
+        const int32_t parts = c1 - c0 + 1;
+#pragma unroll
+        for (int i = 0; i < 2 * NT; ++i) {
+          (&big[0][0])[i] = -INFINITY;
+          (&sum[0][0])[i] = 0.0f;
+        }
+        for (int32_t k = 0; k < parts; ++k) {
+          const float* d = slot_of(c0 + k);
+#pragma unroll
+          for (int i = 0; i < 2 * NT; ++i)
+            (&big[0][0])[i] = fmaxf((&big[0][0])[i], __ldcg(d + (NO + i) * 32));
+        }
+        // a warp merges its share of dim
+        constexpr int KW = KS / kAttWarps;                // tiles of dim of each piece
+        float acc[HALVES][KW][NT][4];
+#pragma unroll
+        for (int i = 0; i < HALVES * KW * NT * 4; ++i) (&acc[0][0][0][0])[i] = 0.0f;
+        for (int32_t k = 0; k < parts; ++k) {
+          const float* d = slot_of(c0 + k);
+          float f[NT][2];
+#pragma unroll
+          for (int i = 0; i < 2 * NT; ++i) {
+            const float m = __ldcg(d + (NO + i) * 32);
+            (&f[0][0])[i] = m == -INFINITY ? 0.0f : exp2f(m - (&big[0][0])[i]);
+            (&sum[0][0])[i] += (&f[0][0])[i] * __ldcg(d + (NO + 2 * NT + i) * 32);
+          }
+#pragma unroll
+          for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+            for (int kk = 0; kk < KW; ++kk)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  acc[hf][kk][nt][e] +=
+                      f[nt][e & 1] *
+                      __ldcg(d + (((hf * KS + warp * KW + kk) * NT + nt) * 4 + e) * 32);
+        }
+#pragma unroll
+        for (int w = 0; w < kAttWarps; ++w)
+          if (w == warp) {
+#pragma unroll
+            for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+              for (int kk = 0; kk < KW; ++kk)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[hf][w * KW + kk][nt][e] = acc[hf][kk][nt][e];
+            write(w * KW, (w + 1) * KW);
+          }
+        if (tid == 0) p.counters[c0] = 0;                 // as the next call finds it
+      }
+      __syncthreads();
+    }
+    fresh = true;
+    if (u + 1 < units) step(at);
+  }
+  if (bad) set_error(p.err, bad);
+}
+
+template <int D, int NT>
+constexpr size_t attend_smem() {
+  constexpr int NO = D / 16 * NT * 4;
+  return (size_t)kAttWarps * kAttStages * stage_bytes<D>() +
+         (size_t)(kAttWarps / 2) * (NO + 2 * NT) * 32 * 4;
+}
+
+// CTAs of a launch: as many as run at once.
+template <int D, int NT, int FMT>
+hs_status residents(int& ctas) {
+  static std::atomic<int> per_sm[kMaxDeviceOrdinals];
+  const int dev = device_ordinal();
+  int n = dev >= 0 ? per_sm[dev].load(std::memory_order_acquire) : 0;
+  if (n == 0) {
+    const auto kernel = kv_attend_kernel<D, NT, FMT>;
+    constexpr int smem = (int)attend_smem<D, NT>();
+    if (const hs_status st = cuda_fail(
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem),
+            "kv_attend shared memory"))
+      return st;
+    if (const hs_status st = cuda_fail(
+            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kAttThreads, smem),
+            "kv_attend occupancy"))
+      return st;
+    if (n < 1) return fail(HS_ERR_CUDA, "kv_attend does not fit an SM");
+    if (n > kAttendMaxPerSm) n = kAttendMaxPerSm;
+    if (dev >= 0) per_sm[dev].store(n, std::memory_order_release);
+  }
+  ctas = n * num_sms();
+  return HS_OK;
+}
+
+template <int D, int NT, int FMT>
+hs_status launch(const AttendParams& p, cudaStream_t stream) {
+  int ctas = 0;
+  if (const hs_status st = residents<D, NT, FMT>(ctas)) return st;
+  launch_pdl(kv_attend_kernel<D, NT, FMT>, dim3((unsigned)ctas), dim3(kAttThreads),
+             attend_smem<D, NT>(), stream, p);
+  count_launches(1);
+  return cuda_fail(cudaGetLastError(), "kv_attend launch");
+}
+
+template <int D, int FMT>
+hs_status launch_rows(const AttendParams& p, int64_t rows, cudaStream_t stream) {
+  if (rows <= 8) return launch<D, 1, FMT>(p, stream);
+  return launch<D, 2, FMT>(p, stream);
+}
+
+template <int FMT>
+hs_status launch_dim(const AttendParams& p, int32_t dim, int64_t rows, cudaStream_t stream) {
+  return dim == 64    ? launch_rows<64, FMT>(p, rows, stream)
+         : dim == 128 ? launch_rows<128, FMT>(p, rows, stream)
+                      : launch_rows<256, FMT>(p, rows, stream);
+}
+
+}  // namespace
+
+// A slot holds (rows x dim) sums, and a maximum and a sum for each lane's rows.
+size_t attend_workspace(int32_t dim) {
+  constexpr int nt = 2;
+  const int64_t ctas = (int64_t)num_sms() * kAttendMaxPerSm;
+  const int64_t slot = ((int64_t)dim / 16 * nt * 4 + 4 * nt) * 32 * 4;
+  return (size_t)(attend_counter_bytes() + ctas * 2 * slot);
+}
+
+hs_status launch_kv_attend(AttendParams p, int32_t dim, int32_t format, int64_t rows, void* ws,
+                           cudaStream_t stream) {
+  p.err = device_error_word();
+  if (!p.err) return fail(HS_ERR_CUDA, "could not resolve the device error word");
+  p.counters = static_cast<unsigned*>(ws);
+  p.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + attend_counter_bytes());
+  p.rows_most = 0x7fffffff;
+  return format == HS_KV_E4M3 ? launch_dim<HS_KV_E4M3>(p, dim, rows, stream)
+                              : launch_dim<HS_KV_INT8>(p, dim, rows, stream);
+}
+
+}  // namespace hs

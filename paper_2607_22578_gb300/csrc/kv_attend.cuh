@@ -1,0 +1,113 @@
+// What the kernels of hs_kv_attend share: their arguments, a request's place, 16-bit values.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "hs_internal.cuh"
+
+namespace hs {
+
+struct AttendParams {
+  const uint8_t* k;
+  const uint8_t* v;
+  const float* ks;
+  const float* vs;
+  int32_t n_blocks;
+  int32_t H;                 // kv heads
+  int32_t G;                 // query heads of each
+  int32_t bt_log2;
+  const uint16_t* q;
+  int64_t q_token, q_head;   // strides, in elements
+  int32_t q_vec;             // rows of q are 16-byte aligned
+  int32_t fp16;
+  int32_t n_tokens;
+  int32_t max_q;
+  const int32_t* lens;
+  const int32_t* starts;     // or NULL: max_q queries each
+  int32_t n_req;
+  const int32_t* n_req_dev;
+  const int32_t* table;
+  int32_t width;
+  int32_t causal;
+  int32_t window;
+  int32_t rows_most;         // requests with more rows (queries times G) are another kernel's
+  float scale_log2;          // scale * log2(e)
+  uint16_t* out;
+  float* lse;
+  unsigned* counters;
+  float* partial;
+  unsigned* err;
+};
+
+constexpr int kAttendMaxPerSm = 4;  // CTAs of a launch that one SM holds, at most
+
+inline int64_t attend_counter_bytes() {
+  return ((int64_t)num_sms() * kAttendMaxPerSm * 4 + 255) / 256 * 256;
+}
+
+// Request r's queries (n of them, from token q0 of the batch) and tokens in the cache; false if
+// it has none, or its numbers cannot be (*bad).
+__device__ __forceinline__ bool attend_request(const AttendParams& p, int32_t r, int32_t& n,
+                                               int32_t& q0, int32_t& len, unsigned* bad) {
+  if (p.starts) {
+    q0 = __ldg(p.starts + r);
+    const int64_t m = (int64_t)__ldg(p.starts + r + 1) - q0;
+    n = (int32_t)(m < -1 ? -1 : (m > 0x7fffffffLL ? 0x7fffffffLL : m));
+  } else {
+    n = p.max_q;
+    q0 = r * p.max_q;
+  }
+  len = __ldg(p.lens + r);
+  if (n == 0) return false;
+  if (n < 0 || n > p.max_q || q0 < 0 || q0 > p.n_tokens - n || len < 0 ||
+      len > ((int64_t)p.width << p.bt_log2)) {
+    *bad = kErrInvalidArg;
+    return false;
+  }
+  return true;
+}
+
+// 8 values of 16 bits as floats
+__device__ __forceinline__ void attend_load8(const uint16_t* src, int vec, int fp16,
+                                             float (&f)[8]) {
+  uint32_t w[4];
+  if (vec) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(src));
+    w[0] = v.x;
+    w[1] = v.y;
+    w[2] = v.z;
+    w[3] = v.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      w[i] = (uint32_t)__ldg(src + 2 * i) | ((uint32_t)__ldg(src + 2 * i + 1) << 16);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (fp16) {
+      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = t.x;
+      f[2 * i + 1] = t.y;
+    } else {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+}
+
+// Two neighbouring outputs, rounded to nearest even
+__device__ __forceinline__ uint32_t attend_pack2(int fp16, float x0, float x1) {
+  if (fp16) {
+    const __half2 h = __floats2half2_rn(x0, x1);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x0, x1);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+__device__ __forceinline__ void attend_store2(uint16_t* dst, int fp16, float x0, float x1) {
+  *reinterpret_cast<uint32_t*>(dst) = attend_pack2(fp16, x0, x1);
+}
+
+}  // namespace hs

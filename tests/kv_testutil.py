@@ -99,3 +99,61 @@ def tables(have, fresh, table, pool, cursor, bt, max_tokens):
 
 def to_bytes(t: torch.Tensor) -> np.ndarray:
     return t.view(torch.uint8).cpu().numpy()
+
+
+def attend(q, k, v, ks, vs, fmt, table, lens, starts, scale, causal, window):
+    """(out, lse, tol_out, tol_lse) in float64 on q's device, one request after the other.
+
+    The tolerances bound what the arithmetic of 16-bit products with fp32 sums
+    may differ by.  With a = sum_j p_j |v_j| (p normalised) and S the largest
+    scale * sum_t |q_t k_jt| of a row:
+      scores: fp32 sums of up to 256 products, q to 2^-24 of its row's largest
+              -> 2^-18 S; the same for lse, with 2^-20 of itself for exp and log
+      weights: rounded to half, 2^-11 each, and what is below 2^-31 of the
+              largest is dropped -> (2^-11 + 2 * 2^-18 S) a + L 2^-31 max|v|,
+              and 2^-14 a for block scales, sums and the division
+    (the output's own rounding is the caller's to add)."""
+    dev = q.device
+    T, Hq, d = q.shape
+    H = k.shape[1]
+    G = Hq // H
+    lut = torch.from_numpy(e4m3_values()).to(dev)
+
+    def val(c, s, ids):
+        x = lut[c.view(torch.uint8)[ids].long()] if fmt == "e4m3" else c[ids].double()
+        return (x * s[ids].double()[..., None, None]).transpose(0, 1).reshape(H, -1, d)
+
+    out = torch.zeros((T, Hq, d), dtype=torch.float64, device=dev)
+    lse = torch.full((T, Hq), -math.inf, dtype=torch.float64, device=dev)
+    tol, tol_l = torch.zeros_like(out), torch.zeros_like(lse)
+    bt = k.shape[2]
+    for r, L in enumerate(lens):
+        a, b = starts[r], starts[r + 1]
+        n = b - a
+        if n == 0 or L == 0:
+            continue
+        ids = table[r, :-(-L // bt)].long()
+        K, V = val(k, ks, ids)[:, :L], val(v, vs, ids)[:, :L]
+        i = torch.arange(n, device=dev)[:, None] + (L - n)
+        j = torch.arange(L, device=dev)[None]
+        see = torch.ones((n, L), dtype=torch.bool, device=dev)
+        if causal:
+            see &= j <= i
+        if window:
+            see &= j > i - window
+        for h in range(Hq):
+            x = q[a:b, h].double()
+            s = (x @ K[h // G].T * scale).masked_fill(~see, -math.inf)
+            m = s.amax(1, keepdim=True)
+            p = torch.where(see, torch.exp(s - torch.where(m == -math.inf, 0.0, m)), 0.0)
+            l = p.sum(1, keepdim=True)
+            p = torch.where(l > 0, p / l, 0.0)
+            vh = torch.where(see.any(0)[:, None], V[h // G], 0.0)
+            out[a:b, h] = p @ vh
+            lse[a:b, h] = torch.where(l > 0, m + l.log(), -math.inf)[:, 0]
+            S = torch.where(see, x.abs() @ K[h // G].abs().T * abs(scale), 0.0).amax(1, keepdim=True)
+            A = p @ vh.abs()
+            tol[a:b, h] = (2.0 ** -11 + 2.0 ** -17 * S + 2.0 ** -14) * A + \
+                L * 2.0 ** -31 * vh.abs().amax()
+            tol_l[a:b, h] = (2.0 ** -18 * S[:, 0] + 2.0 ** -20 * (1 + lse[a:b, h].abs())).nan_to_num()
+    return out, lse, tol, tol_l

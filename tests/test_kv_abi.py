@@ -75,6 +75,40 @@ def test_append_refuses(bad):
     assert append(cache(), **bad) == _lib.HS_ERR_INVALID_ARG and message()
 
 
+def attend(c=None, q=A, dtype=0, T=4, heads=8, lens=A, starts=A, n=4, n_dev=None, max_q=1, table=A,
+           width=8, scale=1.0, causal=1, window=0, out=A, lse=A, ws=A, size=1 << 30):
+    c = cache() if c is None else c
+    return status("hs_kv_attend", ctypes.addressof(c), q, dtype, T, heads, heads * 128, 128, lens,
+                  starts, n, n_dev, max_q, table, width, scale, causal, window, out, lse, ws, size,
+                  None)
+
+
+@pytest.mark.parametrize("bad,what", [
+    (dict(heads=0), "n_heads"), (dict(heads=7), "n_heads"), (dict(T=-1), "n_tokens"),
+    (dict(max_q=-1), "max_q"), (dict(max_q=1 << 30), "max_q"), (dict(T=1 << 29), "n_tokens"),
+    (dict(starts=None, T=3), "starts"), (dict(width=0), "table_width"),
+    (dict(width=(1 << 27) - 1), "table_width"), (dict(window=-1), "window"),
+    (dict(window=3, causal=0), "window"), (dict(scale=0.0), "scale"), (dict(scale=-1.0), "scale"),
+    (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"),
+    (dict(dtype=5), "dtype"), (dict(q=None), "NULL"), (dict(lens=None), "NULL"),
+    (dict(table=None), "NULL"), (dict(out=None), "NULL"), (dict(q=A + 1), "misaligned"),
+    (dict(out=A + 8), "misaligned"), (dict(lse=A + 2), "misaligned"), (dict(n=-1), "n_req"),
+])
+def test_attend_refuses(bad, what):
+    assert attend(**bad) == _lib.HS_ERR_INVALID_ARG and what in message()
+
+
+def test_attend_workspace():
+    for ws, size in ((None, 1 << 30), (A + 16, 1 << 30), (A, 1024)):
+        assert attend(ws=ws, size=size) == _lib.HS_ERR_WORKSPACE
+    need = _lib.load().hs_kv_attend_workspace
+    assert need(8, 2, 128, 1) > 0
+    for bad in ((0, 2, 128, 1), (8, 3, 128, 1), (8, 2, 96, 1), (8, 2, 128, -1)):
+        assert need(*bad) == 0
+
+
 def test_nothing_to_do():
+    for none in (dict(n=0), dict(T=0, max_q=0), dict(max_q=0)):
+        assert attend(q=None, lens=None, table=None, out=None, ws=None, **none) == _lib.HS_OK
     assert append(cache(), T=0, k=None, v=None, slots=None) == _lib.HS_OK
     assert append(None) == _lib.HS_ERR_INVALID_ARG and "cache" in message()
