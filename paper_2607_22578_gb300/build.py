@@ -19,7 +19,7 @@ LIB = os.path.join(PKG, "libhs.so")
 SOURCES = ["api.cu", "fingerprint.cu", "unique.cu", "scatter.cu", "retrieve.cu",
            "query_merge.cu", "segment_sum.cu", "rerank.cu",
            "result_cache.cu", "kv_tables.cu", "kv_append.cu",
-           "kv_attend.cu", "diag.cu"]
+           "kv_attend.cu", "kv_attend_tiles.cu", "diag.cu"]
 HEADERS = [os.path.join(CSRC, h) for h in ("hs_internal.cuh", "fnv.cuh", "fnv_warp.cuh", "row_table.cuh",
                                              "kv_cache.cuh", "kv_attend.cuh")] + \
     [os.path.join(ROOT, "include", "hs.h")]

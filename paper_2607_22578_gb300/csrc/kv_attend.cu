@@ -27,6 +27,9 @@
 #include "kv_attend.cuh"
 
 namespace hs {
+
+hs_status launch_kv_attend_tiles(const AttendParams&, int32_t, int32_t, cudaStream_t);
+
 namespace {
 
 constexpr int kAttWarps = 4;
@@ -34,6 +37,7 @@ constexpr int kAttThreads = kAttWarps * 32;
 constexpr int kWarpTokens = 32;                          // of a unit, for each warp
 constexpr int kUnitTokens = kAttWarps * kWarpTokens;
 constexpr int kAttStages = 2;
+constexpr int kFewRows = 32;                             // of a request: more are kv_attend_tiles.cu's
 constexpr float kLag = 8.0f;                             // of the running maximum, in powers of two
 constexpr float kShift = 7.0f;
 
@@ -749,6 +753,13 @@ hs_status launch_kv_attend(AttendParams p, int32_t dim, int32_t format, int64_t 
   p.counters = static_cast<unsigned*>(ws);
   p.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + attend_counter_bytes());
   p.rows_most = 0x7fffffff;
+  if (dim <= 128 && rows > kFewRows) {
+    // Requests of many rows by tiles; with lengths of their own there may be others.
+    p.rows_most = kFewRows;
+    if (const hs_status st = launch_kv_attend_tiles(p, dim, format, stream)) return st;
+    if (!p.starts) return HS_OK;
+    rows = kFewRows;
+  }
   return format == HS_KV_E4M3 ? launch_dim<HS_KV_E4M3>(p, dim, rows, stream)
                               : launch_dim<HS_KV_INT8>(p, dim, rows, stream);
 }

@@ -114,6 +114,27 @@ def test_heads(H, G, d):
     both(problem([77, 3, 260], [2, 3, 40], H, G, d, 32, "int8", "bf16"))
 
 
+@pytest.mark.parametrize("d,bt,H,G", [(128, 16, 2, 4), (64, 32, 3, 1), (128, 128, 1, 8),
+                                      (64, 64, 1, 5), (256, 32, 1, 4)])
+@pytest.mark.parametrize("fmt,dtype", [("e4m3", "bf16"), ("int8", "fp16")])
+def test_prompts(d, bt, H, G, fmt, dtype):
+    """Whole prompts, chunks at the end of longer ones, and single tokens beside them."""
+    both(problem([513, 300, 1, 64, 129], [513, 300, 1, 64, 129], H, G, d, bt, fmt, dtype))
+    both(problem([1500, 1027, 640, 260], [33, 260, 1, 127], H, G, d, bt, fmt, dtype))
+    both(problem([700, 45, 0, 390], [1, 200, 64, 257], H, G, d, bt, fmt, dtype), causal=False)
+
+
+def test_more_prompts_than_sms():
+    """Several prompts one after the other on each SM, of one and of two tiles of rows, and more
+    requests than threads."""
+    rng = np.random.default_rng(8)
+    n = rng.integers(0, 130, size=500)
+    have = rng.integers(0, 300, size=500)
+    both(problem((have + n).tolist(), n.tolist(), 2, 3, 64, 16, "e4m3", "bf16"))
+    n = rng.integers(20, 90, size=90)
+    both(problem((n + 5).tolist(), n.tolist(), 4, 4, 128, 32, "int8", "bf16"))
+
+
 @pytest.mark.parametrize("causal,window", [(True, 1), (True, 16), (True, 100), (True, 1000),
                                            (True, 2**31 - 1), (False, 0)])
 @pytest.mark.parametrize("n", [1, 7, 150])
