@@ -68,21 +68,17 @@ __device__ __forceinline__ bool attend_request(const AttendParams& p, int32_t r,
   return true;
 }
 
-// 8 values of 16 bits as floats
-__device__ __forceinline__ void attend_load8(const uint16_t* src, int vec, int fp16,
-                                             float (&f)[8]) {
+// 8 values of 16 bits that are only 2-byte aligned
+__device__ __forceinline__ uint4 attend_raw8(const uint16_t* src) {
   uint32_t w[4];
-  if (vec) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4*>(src));
-    w[0] = v.x;
-    w[1] = v.y;
-    w[2] = v.z;
-    w[3] = v.w;
-  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = (uint32_t)__ldg(src + 2 * i) | ((uint32_t)__ldg(src + 2 * i + 1) << 16);
-  }
+  for (int i = 0; i < 4; ++i)
+    w[i] = (uint32_t)__ldg(src + 2 * i) | ((uint32_t)__ldg(src + 2 * i + 1) << 16);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ void attend_unpack8(const uint4& v, int fp16, float (&f)[8]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     if (fp16) {
@@ -94,6 +90,12 @@ __device__ __forceinline__ void attend_load8(const uint16_t* src, int vec, int f
       f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
+}
+
+// 8 values of 16 bits as floats
+__device__ __forceinline__ void attend_load8(const uint16_t* src, int vec, int fp16,
+                                             float (&f)[8]) {
+  attend_unpack8(vec ? __ldg(reinterpret_cast<const uint4*>(src)) : attend_raw8(src), fp16, f);
 }
 
 // Two neighbouring outputs, rounded to nearest even

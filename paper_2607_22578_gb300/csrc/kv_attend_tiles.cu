@@ -8,10 +8,11 @@
 // keeps two tiles of rows in flight that take turns: while one's scores become weights, the tensor
 // cores work for the other.
 //
-//   warps 0-3, 4-7   a thread a row: scores to weights, the output at the end
-//   warps 8-11       queries, and codes from the cache's blocks, decoded to half in shared memory
-//                    (swizzled; K and V alike: K is read along dim, V across it)
-//   warp 12          one thread issues every product
+//   warps 0-3, 4-7   a thread a row: its query into shared memory, scores to weights, the output
+//   warps 8-10       codes from the cache's blocks, decoded to half in shared memory (swizzled;
+//                    K and V alike: K is read along dim, V across it), a tile ahead in registers
+//   warp 11          one thread issues every product
+// Twelve warps, so that a thread may have 168 registers: a row's 128 scores stay in them.
 //
 // CTAs are persistent, one an SM.  Work is (request, pair of tiles of rows, kv head) items, the
 // later pairs of a request (which see more) first; an item's queries and first tokens are loaded
@@ -33,11 +34,13 @@ constexpr int kPairRows = 2 * kTileRows;
 constexpr int kTileTokens = 128;
 constexpr int kGroups = kTileTokens / 16;      // 16 tokens lie in one block: one scale
 constexpr int kSoftWarps = 8;
-constexpr int kLoadWarp = 8;                   // the first of four
-constexpr int kMmaWarp = 12;
-constexpr int kTilesThreads = 13 * 32;
-constexpr int kLoadThreads = 128;
-constexpr int kScaleRing = 4;
+constexpr int kLoadWarp = 8;                   // the first of three
+constexpr int kLoadWarps = 3;
+constexpr int kMmaWarp = 11;
+constexpr int kTilesThreads = 12 * 32;
+constexpr int kLoadThreads = kLoadWarps * 32;
+constexpr int kScaleRing = 4;                  // tiles
+constexpr int kItemRing = 4;
 constexpr float kTilesLag = 8.0f;
 constexpr float kTilesShift = 7.0f;
 constexpr float kLeastScale = 1.17549435e-38f;
@@ -60,12 +63,12 @@ struct Item {
 };
 
 struct TilesShared {
-  uint64_t q_full, q_empty;
+  uint64_t item_full[kItemRing], item_empty[kItemRing];
+  uint64_t q_full[2];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
   uint64_t s_full[2], p_full[2], o_full[2];
   uint64_t drained;
-  Item item;
-  float q_scale[kPairRows];
+  Item items[kItemRing];
   float4 scales[kScaleRing][kGroups];   // of 16 tokens: keys', log2 of values', 1 / values'
   uint32_t tmem;
   int abort;
@@ -128,6 +131,32 @@ __device__ __forceinline__ float fast_exp2(float x) {
   return y;
 }
 
+// Two floats at once (sm_100's packed fp32 operations)
+__device__ __forceinline__ uint64_t pack_b32x2(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ uint64_t pack_f32x2(float lo, float hi) {
+  return pack_b32x2(__float_as_uint(lo), __float_as_uint(hi));
+}
+__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
+  uint32_t a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
+  lo = __uint_as_float(a);
+  hi = __uint_as_float(b);
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // The scores' factor; never 0, so that a hidden score's -inf stays one.
 __device__ __forceinline__ float factor(float scale, float q_scale) {
   const float f = scale * q_scale;
@@ -162,9 +191,12 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
 
   if (tid == 0) {
-    mbar_init(&sh.q_full, kLoadThreads);
-    mbar_init(&sh.q_empty, kSoftWarps + 1);
+    for (int i = 0; i < kItemRing; ++i) {
+      mbar_init(&sh.item_full[i], 1);
+      mbar_init(&sh.item_empty[i], kSoftWarps + 1);
+    }
     for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.q_full[i], kTileRows);
       mbar_init(&sh.k_full[i], kLoadThreads);
       mbar_init(&sh.k_empty[i], 1);
       mbar_init(&sh.v_full[i], kLoadThreads);
@@ -222,12 +254,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
   };
 
   if (warp >= kLoadWarp && warp < kMmaWarp) {
-    // ================================ queries, keys and values
-    const int lw = warp - kLoadWarp, lt = tid - kLoadWarp * 32;
-    uint32_t items = 0, tiles = 0;                  // done so far, of this CTA
-    bool ok = true;
-    for (int32_t at = blockIdx.x;; at += gridDim.x, ++items) {
-      Item it{};
+    // ================================ keys and values
+    const int lw = warp - kLoadWarp;
+    const int row8 = lane & 7, chunk = lane >> 3;   // of 8 tokens' 64 bytes
+    constexpr int RG = (kTileTokens / 8 + kLoadWarps - 1) / kLoadWarps;  // groups of 8 tokens, mine
+    constexpr int CH = D / 64;
+
+    // The tiles of this CTA's items end to end.  Of the one looked up (blocks only):
+    Item it{};
+    int32_t at = blockIdx.x, tile = 0;
+    uint32_t items = 0;                             // items said so far
+    bool ok = true, more = true;
+    const auto next_item = [&]() {                  // the next item, for everybody
+      it = Item{};
       it.more = at < total;
       if (it.more) {
         int lo = 0, hi = kTilesThreads;             // the last thread with before <= at
@@ -249,166 +288,146 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         const int32_t see = p.causal ? min(it.len, it.len - it.n + i1 + 1) : it.len;
         const int32_t from = p.window > 0 ? max(0, it.len - it.n + i0 - p.window + 1) : 0;
         it.tile0 = from / kTileTokens;
-        it.tiles = max(0, (see + kTileTokens - 1) / kTileTokens - it.tile0);
+        it.tiles = (see + kTileTokens - 1) / kTileTokens - it.tile0;
+        if (it.tiles < 1) {                         // nothing is seen: one tile, hidden
+          it.tile0 = 0;
+          it.tiles = 1;
+        }
+        at += gridDim.x;
       }
-      if (items > 0 && !(ok = wait(&sh.q_empty, items - 1))) break;
-      if (lt == 0) sh.item = it;
-      if (!it.more) {
-        mbar_arrive(&sh.q_full);
-        break;
+      const uint32_t slot = items & (kItemRing - 1);
+      if (items >= kItemRing) ok = ok && wait(&sh.item_empty[slot], items / kItemRing - 1);
+      if (lw == 0 && lane == 0 && ok) {
+        sh.items[slot] = it;
+        mbar_arrive(&sh.item_full[slot]);
       }
+      ++items;
+      more = it.more;
+      tile = it.tile0;
+    };
 
-      // the tokens' codes are on their way while the queries are laid out
-      constexpr int CH = D / 64;                    // loads of 64 bytes of a token's codes
-      const int row8 = lane & 7, chunk = lane >> 3;
-      uint4 kr[4][CH], vr[4][CH];
-      float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
-      int32_t ids[2];
-      const auto look_up = [&](int32_t t) {         // the blocks of this warp's 32 tokens
-        const int32_t t0 = (it.tile0 + t) * kTileTokens + lw * 32;
-        const int32_t* row = p.table + (int64_t)it.r * p.width;
+    int32_t ids[RG], t_len = 0, t_h = 0, t_0 = 0;   // of the tile that is fetched next
+    int32_t sid = -1;
+    const auto look_up = [&]() {                    // its blocks, and one tile on
+      t_len = it.len;
+      t_h = it.h;
+      t_0 = tile * kTileTokens;
+      const int32_t* row = p.table + (int64_t)it.r * p.width;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int32_t tok = t0 + i * 16;
-          ids[i] = tok < it.len ? __ldg(row + (tok >> p.bt_log2)) : -1;
-          if (tok < it.len && (uint32_t)ids[i] >= (uint32_t)p.n_blocks) {
-            bad = kErrInvalidArg;
-            ids[i] = -1;
+      for (int i = 0; i < RG; ++i) {
+        const int32_t g = lw + i * kLoadWarps, tok = t_0 + g * 8;
+        ids[i] = g < kTileTokens / 8 && tok < t_len ? __ldg(row + (tok >> p.bt_log2)) : -1;
+      }
+      if (lw == 0 && lane < kGroups)
+        sid = t_0 + lane * 16 < t_len ? __ldg(row + ((t_0 + lane * 16) >> p.bt_log2)) : -1;
+      if (++tile == it.tile0 + it.tiles) next_item();
+    };
+    uint4 kr[RG][CH], vr[RG][CH];
+    float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
+    const auto fetch = [&](const uint8_t* codes, uint4 (&to)[RG][CH]) {
+#pragma unroll
+      for (int i = 0; i < RG; ++i) {
+        const int32_t tok = t_0 + (lw + i * kLoadWarps) * 8 + row8, id = ids[i];
+        const bool known = (uint32_t)id < (uint32_t)p.n_blocks;
+        const bool in = tok < t_len && known;
+        if (id != -1 && !known) bad = kErrInvalidArg;
+        const uint8_t* src =
+            codes + (((((int64_t)(in ? id : 0) * p.H + t_h) << p.bt_log2) +
+                      (tok & ((1 << p.bt_log2) - 1))) * D) + chunk * 16;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+          to[i][c] = in ? __ldg(reinterpret_cast<const uint4*>(src + c * 64))
+                        : make_uint4(0u, 0u, 0u, 0u);
+      }
+    };
+    const auto fetch_scale = [&]() {
+      if (lw == 0 && lane < kGroups) {
+        const bool in = (uint32_t)sid < (uint32_t)p.n_blocks;
+        if (!in && t_0 + lane * 16 < t_len) bad = kErrInvalidArg;
+        const float a = in ? __ldg(p.ks + (int64_t)sid * p.H + t_h) : 0.0f;
+        const float b = in ? __ldg(p.vs + (int64_t)sid * p.H + t_h) : 0.0f;
+        sc = make_float4(a, b, 0.f, 0.f);
+      }
+    };
+    const auto put = [&](uint32_t to, const uint4 (&from)[RG][CH]) {
+#pragma unroll
+      for (int i = 0; i < RG; ++i) {
+        const int g = lw + i * kLoadWarps;
+        if (g >= kTileTokens / 8) break;
+        const int row = g * 8 + row8;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+          const uint32_t w[4] = {from[i][c].x, from[i][c].y, from[i][c].z, from[i][c].w};
+          uint32_t h[8];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            h[2 * e] = KvFormat<FMT>::template decode2<0>(w[e]);
+            h[2 * e + 1] = KvFormat<FMT>::template decode2<1>(w[e]);
           }
+          const uint32_t line = to + c * L::kBlockBytes + row * 128;
+          sts128(line + (((2 * chunk) ^ row8) << 4), h[0], h[1], h[2], h[3]);
+          sts128(line + (((2 * chunk + 1) ^ row8) << 4), h[4], h[5], h[6], h[7]);
         }
-      };
-      const auto fetch = [&](const uint8_t* codes, int32_t t, uint4 (&to)[4][CH]) {
-        const int32_t t0 = (it.tile0 + t) * kTileTokens + lw * 32;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int32_t tok = t0 + g * 8 + row8, id = ids[g >> 1];
-          const bool in = tok < it.len && id >= 0;
-          const uint8_t* src =
-              codes + (((((int64_t)(in ? id : 0) * p.H + it.h) << p.bt_log2) +
-                        (tok & ((1 << p.bt_log2) - 1))) * D) + chunk * 16;
-#pragma unroll
-          for (int c = 0; c < CH; ++c)
-            to[g][c] = in ? __ldg(reinterpret_cast<const uint4*>(src + c * 64))
-                          : make_uint4(0u, 0u, 0u, 0u);
-        }
-      };
-      const auto fetch_scale = [&]() {
-        if (lane < 2) {
-          const int32_t id = lane ? ids[1] : ids[0];
-          const float a = id >= 0 ? __ldg(p.ks + (int64_t)id * p.H + it.h) : 0.0f;
-          const float b = id >= 0 ? __ldg(p.vs + (int64_t)id * p.H + it.h) : 0.0f;
-          const float v = b < kLeastScale ? kLeastScale : b;      // (a NaN stays one)
-          sc = make_float4(a < kLeastScale ? kLeastScale : a, log2f(v), __fdividef(1.0f, v), 0.f);
-        }
-      };
-      const auto put = [&](uint32_t to, const uint4 (&from)[4][CH]) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int row = lw * 32 + g * 8 + row8;
-#pragma unroll
-          for (int c = 0; c < CH; ++c) {
-            const uint32_t w[4] = {from[g][c].x, from[g][c].y, from[g][c].z, from[g][c].w};
-            uint32_t h[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              h[2 * i] = KvFormat<FMT>::template decode2<0>(w[i]);
-              h[2 * i + 1] = KvFormat<FMT>::template decode2<1>(w[i]);
-            }
-            const uint32_t line = to + c * L::kBlockBytes + row * 128;
-            sts128(line + (((2 * chunk) ^ row8) << 4), h[0], h[1], h[2], h[3]);
-            sts128(line + (((2 * chunk + 1) ^ row8) << 4), h[4], h[5], h[6], h[7]);
-          }
-        }
-      };
-      if (it.tiles > 0) {
-        look_up(0);
-        fetch(p.k, 0, kr);
-        fetch(p.v, 0, vr);
+      }
+    };
+    next_item();
+    bool fetched = more && ok;
+    if (fetched) {
+      look_up();
+      fetch(p.k, kr);
+      fetch(p.v, vr);
+      fetch_scale();
+    }
+    bool looked = more && ok;
+    if (fetched && looked) look_up();
+    for (uint32_t n = 0; fetched && ok; ++n) {
+      const uint32_t st = n & 1, use = n >> 1;
+      if (n >= 2 && !(ok = wait(&sh.k_empty[st], use - 1))) break;
+      if (lw == 0 && lane < kGroups) {
+        const float v = sc.y < kLeastScale ? kLeastScale : sc.y;  // (a NaN stays one)
+        sh.scales[n & (kScaleRing - 1)][lane] =
+            make_float4(sc.x < kLeastScale ? kLeastScale : sc.x, log2f(v), __fdividef(1.0f, v), 0.f);
+      }
+      put(base + L::kK + st * L::kTileBytes, kr);
+      fence_async_shared();
+      mbar_arrive(&sh.k_full[st]);
+      if (looked) {
+        fetch(p.k, kr);
         fetch_scale();
       }
-      // queries: D / 8 lanes a row, 8 values each
-      {
-        constexpr int LR = D / 8, RS = 32 / LR;     // lanes of a row, rows of a step
-        constexpr int UN = 4;
-        const int32_t rows = min(it.rows - it.rows0, kPairRows);
-        for (int s = lw * RS; s < kPairRows; s += 4 * RS * UN) {
-          float f[UN][8];
-#pragma unroll
-          for (int u = 0; u < UN; ++u) {
-            const int row = s + u * 4 * RS + lane / LR;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[u][e] = 0.0f;
-            if (row < rows) {
-              const int32_t full = it.rows0 + row, i = full / p.G, j = full - i * p.G;
-              attend_load8(p.q + (int64_t)(it.q0 + i) * p.q_token +
-                               (int64_t)(it.h * p.G + j) * p.q_head + (lane % LR) * 8,
-                           p.q_vec, p.fp16, f[u]);
-            }
-          }
-#pragma unroll
-          for (int u = 0; u < UN; ++u) {
-            const int row = s + u * 4 * RS + lane / LR;
-            float big = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(f[u][e]));
-#pragma unroll
-            for (int o = 1; o < LR; o <<= 1)
-              big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-            const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
-            const float by = __uint_as_float((254u - e) << 23);
-            const int ch = lane % LR;               // 16-byte chunk of the row
-            const uint32_t line = base + L::kQ + (row >> 7) * L::kTileBytes +
-                                  (ch >> 3) * L::kBlockBytes + (row & 127) * 128;
-            sts128(line + (((ch ^ row) & 7) << 4), half2_of(f[u][0] * by, f[u][1] * by),
-                   half2_of(f[u][2] * by, f[u][3] * by), half2_of(f[u][4] * by, f[u][5] * by),
-                   half2_of(f[u][6] * by, f[u][7] * by));
-            if (ch == 0) sh.q_scale[row] = __uint_as_float(e << 23) * p.scale_log2;
-          }
-        }
-      }
+      if (n >= 2 && !(ok = wait(&sh.v_empty[st], use - 1))) break;
+      put(base + L::kV + st * L::kTileBytes, vr);
       fence_async_shared();
-      mbar_arrive(&sh.q_full);
-
-      for (int32_t t = 0; t < it.tiles && ok; ++t, ++tiles) {
-        const uint32_t st = tiles & 1, use = tiles >> 1;
-        if (tiles >= 2 && !(ok = wait(&sh.k_empty[st], use - 1))) break;
-        if (lane < 2) sh.scales[tiles & (kScaleRing - 1)][lw * 2 + lane] = sc;
-        put(base + L::kK + st * L::kTileBytes, kr);
-        fence_async_shared();
-        mbar_arrive(&sh.k_full[st]);
-        if (t + 1 < it.tiles) {
-          look_up(t + 1);
-          fetch(p.k, t + 1, kr);
-          fetch_scale();
-        }
-        if (tiles >= 2 && !(ok = wait(&sh.v_empty[st], use - 1))) break;
-        put(base + L::kV + st * L::kTileBytes, vr);
-        fence_async_shared();
-        mbar_arrive(&sh.v_full[st]);
-        if (t + 1 < it.tiles) fetch(p.v, t + 1, vr);
-      }
-      if (!ok) break;
+      mbar_arrive(&sh.v_full[st]);
+      if (looked) fetch(p.v, vr);
+      fetched = looked;
+      looked = more && looked;
+      if (looked) look_up();
     }
   } else if (warp == kMmaWarp) {
     // ================================ products
     if (lane == 0) {
       constexpr uint32_t id_qk = idesc_f16(kTileRows, kTileTokens, false);
       constexpr uint32_t id_pv = idesc_f16(kTileRows, D, true);
-      uint32_t tiles = 0, np[2] = {0, 0};
+      const uint64_t d_q = smem_desc_k_sw128(base + L::kQ);
+      const uint64_t d_k = smem_desc_k_sw128(base + L::kK);
+      const uint64_t d_v = smem_desc_mn_sw128(base + L::kV, L::kBlockBytes);
+      uint32_t tiles = 0, np[2] = {0, 0}, nq1 = 0;
       const auto qk = [&](int x, uint32_t st) {
+        const uint64_t a = d_q + (x * L::kTileBytes >> 4), b = d_k + (st * L::kTileBytes >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (k >> 2) * L::kBlockBytes + (k & 3) * 32;
-          umma_ss(tmem + x * kTileTokens, smem_desc_k_sw128(base + L::kQ + x * L::kTileBytes + off),
-                  smem_desc_k_sw128(base + L::kK + st * L::kTileBytes + off), id_qk, k > 0);
+          constexpr int kPerBlock = 4;
+          const int off = ((k / kPerBlock) * L::kBlockBytes + (k % kPerBlock) * 32) >> 4;
+          umma_ss(tmem + x * kTileTokens, a + off, b + off, id_qk, k > 0);
         }
       };
       const auto pv = [&](int x, uint32_t st, bool add) {
+        const uint64_t b = d_v + (st * L::kTileBytes >> 4);
 #pragma unroll
         for (int k = 0; k < kTileTokens / 16; ++k)
           umma_ts(tmem + 2 * kTileTokens + x * D, tmem + x * kTileTokens + k * 8,
-                  smem_desc_mn_sw128(base + L::kV + st * L::kTileBytes + k * 2048, L::kBlockBytes),
-                  id_pv, add || k > 0);
+                  b + (k * 2048 >> 4), id_pv, add || k > 0);
       };
       // The arrival of this thread's own passes on what it has seen: the block scales.
       const auto scored = [&](int x) {
@@ -417,16 +436,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       };
       bool ok = true;
       for (uint32_t items = 0; ok; ++items) {
-        if (!(ok = wait_one(&sh.q_full, items))) break;
-        tc_fence_after();
-        const Item it = sh.item;
-        if (!it.more) break;
-        const bool two = it.rows - it.rows0 > kTileRows;
-        if (it.tiles == 0) {
-          mbar_arrive(&sh.q_empty);
-          continue;
-        }
-        for (int32_t t = 0; t < it.tiles; ++t, ++tiles) {
+        const uint32_t slot = items & (kItemRing - 1);
+        if (!(ok = wait_one(&sh.item_full[slot], items / kItemRing))) break;
+        const int32_t n_tiles = sh.items[slot].tiles;
+        const bool two = sh.items[slot].rows - sh.items[slot].rows0 > kTileRows;
+        if (!sh.items[slot].more) break;
+        mbar_arrive(&sh.item_empty[slot]);
+        if (!(ok = wait_one(&sh.q_full[0], items))) break;
+        for (int32_t t = 0; t < n_tiles; ++t, ++tiles) {
           const uint32_t st = tiles & 1, use = tiles >> 1;
           if (!(ok = wait_one(&sh.k_full[st], use))) break;
           tc_fence_after();
@@ -439,12 +456,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
               pv(1, st ^ 1, t > 1);
               umma_commit(&sh.o_full[1]);
               umma_commit(&sh.v_empty[st ^ 1]);
+            } else {
+              if (!(ok = wait_one(&sh.q_full[1], nq1++))) break;
+              tc_fence_after();
             }
             qk(1, st);
             scored(1);
           }
           umma_commit(&sh.k_empty[st]);
-          if (t + 1 == it.tiles) umma_commit(&sh.q_empty);
           if (!(ok = wait_one(&sh.v_full[st], use))) break;
           if (!(ok = wait_one(&sh.p_full[0], np[0]++))) break;
           tc_fence_after();
@@ -457,7 +476,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
           const uint32_t st = (tiles - 1) & 1;
           if (!(ok = wait_one(&sh.p_full[1], np[1]++))) break;
           tc_fence_after();
-          pv(1, st, it.tiles > 1);
+          pv(1, st, n_tiles > 1);
           umma_commit(&sh.o_full[1]);
           umma_commit(&sh.v_empty[st]);
         }
@@ -471,29 +490,73 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     }
     __syncwarp();
   } else {
-    // ================================ scores to weights, and the output
+    // ================================ queries, scores to weights, the output
     const int x = warp >> 2;                        // which tile of rows
     const int row = (warp & 3) * 32 + lane;         // of it, and lane of tensor memory
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t t_s = tmem + lanes + x * kTileTokens;
     const uint32_t t_o = tmem + lanes + 2 * kTileTokens + x * D;
-    uint32_t tiles = 0, ns = 0;                     // of the CTA; of this group
+    const uint32_t q_line = base + L::kQ + x * L::kTileBytes + row * 128;
+    uint32_t items = 0, tiles = 0, ns = 0;          // of the CTA; of this group
     bool ok = true;
-    for (uint32_t items = 0; ok; ++items) {
-      if (!(ok = wait(&sh.q_full, items))) break;
-      const Item it = sh.item;
-      const float qs = sh.q_scale[x * kTileRows + row];
-      __syncwarp();
-      if (!it.more) break;
-      if (lane == 0) mbar_arrive(&sh.q_empty);
-      const int32_t rows0 = it.rows0 + x * kTileRows;
-      if (rows0 >= it.rows) {                       // no rows of this item are this group's
+
+    // The next item that has rows of this group's, and this thread's row of its queries.  Its
+    // place in shared memory is free: the group's last scores are there.
+    Item it{};
+    int32_t rows0 = 0, qi = 0, qj = 0;
+    float qs = 0.0f;
+    const auto take = [&]() {
+      for (;;) {
+        const uint32_t slot = items & (kItemRing - 1);
+        if (!(ok = wait(&sh.item_full[slot], items / kItemRing))) return;
+        it = sh.items[slot];
+        __syncwarp();
+        if (!it.more) return;
+        if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
+        ++items;
+        rows0 = it.rows0 + x * kTileRows;
+        if (rows0 < it.rows) break;
         tiles += it.tiles;
-        continue;
       }
       const int32_t full = min(rows0 + row, it.rows - 1);
-      const int32_t i = full / p.G, j = full - i * p.G;
-      const int32_t pos = it.len - it.n + i;
+      qi = full / p.G;
+      qj = full - qi * p.G;
+      const uint16_t* src = p.q + (int64_t)(it.q0 + qi) * p.q_token +
+                            (int64_t)(it.h * p.G + qj) * p.q_head;
+      uint4 v[D / 8];
+      if (p.q_vec) {
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) v[c] = __ldg(reinterpret_cast<const uint4*>(src) + c);
+      } else {
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) v[c] = attend_raw8(src + c * 8);
+      }
+      float big = 0.0f;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        float f[8];
+        attend_unpack8(v[c], p.fp16, f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(f[e]));
+      }
+      // a power of two of the row's size, kept where it and its inverse are normal
+      const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+      const float by = __uint_as_float((254u - e) << 23);
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        float f[8];
+        attend_unpack8(v[c], p.fp16, f);
+        sts128(q_line + (c >> 3) * L::kBlockBytes + (((c ^ row) & 7) << 4),
+               half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
+               half2_of(f[4] * by, f[5] * by), half2_of(f[6] * by, f[7] * by));
+      }
+      qs = __uint_as_float(e << 23) * p.scale_log2;
+      fence_async_shared();
+      mbar_arrive(&sh.q_full[x]);
+    };
+    take();
+    while (ok && it.more) {
+      const int32_t n_tiles = it.tiles, pos = it.len - it.n + qi;
       const int32_t top = p.causal ? min(pos, it.len - 1) : it.len - 1;
       const int32_t bottom = p.window > 0 ? pos - p.window + 1 : 0;
       // tokens that every row of the tile sees: from .. to
@@ -503,35 +566,31 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       const int32_t from = p.window > 0 ? pos1 - p.window + 1 : 0;
 
       float m = -INFINITY, sum = 0.0f;
-      for (int32_t t = 0; t < it.tiles; ++t, ++tiles, ++ns) {
+      for (int32_t t = 0; t < n_tiles; ++t, ++tiles, ++ns) {
         if (!(ok = wait(&sh.s_full[x], ns))) break;
         tc_fence_after();
         const float4* scales = sh.scales[tiles & (kScaleRing - 1)];
         const int32_t t0 = (it.tile0 + t) * kTileTokens;
-        const bool whole = t0 >= from && t0 + kTileTokens - 1 <= to;
-        const int32_t last = top - t0, first = bottom - t0;
+        uint32_t a[kTileTokens];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          tmem_ld_32x32b_x32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(a + c * 32));
+        tmem_ld_wait();
+        if (t0 < from || t0 + kTileTokens - 1 > to) {
+          const int32_t last = top - t0, first = bottom - t0;
+#pragma unroll
+          for (int e = 0; e < kTileTokens; ++e)
+            if (e > last || e < first) a[e] = 0xff800000u;  // -inf
+        }
         // ---- the maximum of acc * c + lv
         float most = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t a[32];
-          tmem_ld_32x32b_x32(t_s + c * 32, a);
-          tmem_ld_wait();
+        for (int g = 0; g < kGroups; ++g) {
+          float b = -INFINITY;
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float4 sc = scales[c * 2 + g];
-            float b = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float z = __uint_as_float(a[g * 16 + e]);
-              if (!whole) {
-                const int32_t tok = c * 32 + g * 16 + e;
-                if (tok > last || tok < first) z = -INFINITY;
-              }
-              b = fmaxf(b, z);
-            }
-            most = fmaxf(most, fmaf(b, factor(sc.x, qs), sc.y));
-          }
+          for (int e = 0; e < 16; ++e) b = fmaxf(b, __uint_as_float(a[g * 16 + e]));
+          const float4 sc = scales[g];
+          most = fmaxf(most, fmaf(b, factor(sc.x, qs), sc.y));
         }
         const bool grow = most > m + kTilesLag;
         if (__any_sync(0xffffffffu, grow)) {
@@ -544,44 +603,39 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
-              uint32_t a[16];
-              tmem_ld_32x32b_x16(t_o + c * 16, a);
+              uint32_t o[16];
+              tmem_ld_32x32b_x16(t_o + c * 16, o);
               tmem_ld_wait();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) a[e] = __float_as_uint(__uint_as_float(a[e]) * f);
-              tmem_st_32x32b_x16(t_o + c * 16, a);
+              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+              tmem_st_32x32b_x16(t_o + c * 16, o);
             }
-            tmem_st_wait();
           }
         }
         // ---- the weights
         const float shift = m == -INFINITY ? 0.0f : kTilesShift - m;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          uint32_t a[32], w[16];
-          tmem_ld_32x32b_x32(t_s + c * 32, a);
-          tmem_ld_wait();
+          uint32_t w[16];
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             const float4 sc = scales[c * 2 + g];
             const float by = factor(sc.x, qs), add = sc.y + shift;
-            float part = 0.0f;
+            const uint64_t by2 = pack_f32x2(by, by), add2 = pack_f32x2(add, add);
+            uint64_t part = 0;
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-              float z[2];
-#pragma unroll
-              for (int y = 0; y < 2; ++y) {
-                float acc = __uint_as_float(a[g * 16 + e + y]);
-                if (!whole) {
-                  const int32_t tok = c * 32 + g * 16 + e + y;
-                  if (tok > last || tok < first) acc = -INFINITY;
-                }
-                z[y] = fast_exp2(fmaf(acc, by, add));
-                part += z[y];
-              }
-              w[(g * 16 + e) / 2] = half2_of(z[0], z[1]);
+              const int k = c * 32 + g * 16 + e;
+              float z0, z1;
+              unpack_f32x2(fma_f32x2(pack_b32x2(a[k], a[k + 1]), by2, add2), z0, z1);
+              z0 = fast_exp2(z0);
+              z1 = fast_exp2(z1);
+              part = add_f32x2(part, pack_f32x2(z0, z1));
+              w[g * 8 + e / 2] = half2_of(z0, z1);
             }
-            sum = fmaf(part, sc.z, sum);
+            float p0, p1;
+            unpack_f32x2(part, p0, p1);
+            sum = fmaf(p0 + p1, sc.z, sum);
           }
           tmem_st_32x32b_x16(t_s + c * 16, w);
         }
@@ -591,21 +645,20 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       }
       if (!ok) break;
 
-      // ---- the output
+      // ---- the output, after the next item's queries
       const bool mine = rows0 + row < it.rows;
-      const int64_t out_row = (int64_t)(it.q0 + i) * (p.H * p.G) + it.h * p.G + j;
-      const float inv = sum > 0.0f ? __fdividef(1.0f, sum) : (sum == 0.0f ? 0.0f : sum);
-      if (it.tiles > 0) {
-        if (!(ok = wait(&sh.o_full[x], ns - 1))) break;
-        tc_fence_after();
-      }
+      const int64_t out_row = (int64_t)(it.q0 + qi) * (p.H * p.G) + it.h * p.G + qj;
+      const bool none = sum == 0.0f;
+      const float inv = none ? 0.0f : __fdividef(1.0f, sum);
+      const uint32_t last = ns - 1;
+      take();
+      if (!ok || !(ok = wait(&sh.o_full[x], last))) break;
+      tc_fence_after();
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
-        uint32_t a[32];
-        if (it.tiles > 0) {
-          tmem_ld_32x32b_x32(t_o + c * 32, a);
-          tmem_ld_wait();
-        }
+        uint32_t o[32];
+        tmem_ld_32x32b_x32(t_o + c * 32, o);
+        tmem_ld_wait();
         if (mine) {
           uint4* dst = reinterpret_cast<uint4*>(p.out + out_row * D + c * 32);
 #pragma unroll
@@ -613,17 +666,17 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float lo = it.tiles > 0 ? __uint_as_float(a[v * 8 + 2 * e]) * inv : 0.0f;
-              const float hi = it.tiles > 0 ? __uint_as_float(a[v * 8 + 2 * e + 1]) * inv : 0.0f;
-              w[e] = attend_pack2(p.fp16, lo, hi);
+              const float lo = __uint_as_float(o[v * 8 + 2 * e]) * inv;
+              const float hi = __uint_as_float(o[v * 8 + 2 * e + 1]) * inv;
+              w[e] = none ? 0u : attend_pack2(p.fp16, lo, hi);
             }
             dst[v] = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
       }
       if (mine && p.lse)
-        p.lse[out_row] = sum == 0.0f ? -INFINITY
-                                     : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
+        p.lse[out_row] = none ? -INFINITY
+                              : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
       tc_fence_before();
     }
   }
