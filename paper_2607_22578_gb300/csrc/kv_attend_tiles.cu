@@ -1,12 +1,13 @@
 // Attention of many query rows over the paged 8-bit cache (hs_kv_attend): prompts, chunks and
 // cross attention, on the tensor cores.
 //
-// The formula is kv_attend.cu's.  A tile is 128 rows (query, head of the group) against 128
-// tokens: s = q k^T is one tcgen05.mma per 16 of dim (M = 128, N = 128) into tensor memory, o += p v
-// one per 16 tokens (N = dim) with p as its A operand in tensor memory.  4 flops a (row, token, dim)
-// and one exponential a (row, token): tensor cores and exponentials bound it together, so a CTA
-// keeps two tiles of rows in flight that take turns: while one's scores become weights, the tensor
-// cores work for the other.
+// The formula is kv_attend.cu's.  A step is 128 rows (query, head of the group) against 64 tokens:
+// s = q k^T is one tcgen05.mma per 16 of dim (M = 128, N = 64) into tensor memory, o += p v one per
+// 16 tokens (N = dim) with p as its A operand in tensor memory.  4 flops a (row, token, dim) and one
+// exponential a (row, token): tensor cores and exponentials bound it together, so a CTA keeps two
+// tiles of rows going and each has two buffers of scores: the next step's are there when a step's
+// weights are done (with one buffer, of 128 tokens, a tile of rows waits for both products: 5500
+// clocks for 128 tokens, of which the products are 2300).
 //
 //   warps 0-3, 4-7   a thread a row: its query into shared memory, scores to weights, the output
 //   warps 8-10       codes from the cache's blocks, decoded to half in shared memory (swizzled;
@@ -33,6 +34,8 @@ constexpr int kTileRows = 128;
 constexpr int kPairRows = 2 * kTileRows;
 constexpr int kTileTokens = 128;
 constexpr int kGroups = kTileTokens / 16;      // 16 tokens lie in one block: one scale
+constexpr int kStepTokens = 64;                // of scores that are computed at once
+constexpr int kStepGroups = kStepTokens / 16;
 constexpr int kSoftWarps = 8;
 constexpr int kLoadWarp = 8;                   // the first of three
 constexpr int kLoadWarps = 3;
@@ -52,13 +55,15 @@ struct TilesLayout {
   static constexpr int kQ = 0;                               // two tiles
   static constexpr int kK = 2 * kTileBytes;                  // two stages
   static constexpr int kV = 4 * kTileBytes;                  // two stages
-  static constexpr int kEnd = 6 * kTileBytes;
+  static constexpr int kOut = 6 * kTileBytes;                // 2 KB a warp: 32 rows, 32 of dim
+  static constexpr int kEnd = kOut + kSoftWarps * 2048;
   static constexpr int kSmem = kEnd + 1024;                  // the base is aligned to 1024
 };
 
 struct Item {
   int32_t r, h, rows0, n, q0, len;
   int32_t tile0, tiles, rows;        // tiles of tokens; rows of the request
+  int32_t steps0, steps1;            // of 64 tokens, for each tile of rows (0: it has no rows)
   int32_t more;                      // 0: no further item
 };
 
@@ -66,7 +71,11 @@ struct TilesShared {
   uint64_t item_full[kItemRing], item_empty[kItemRing];
   uint64_t q_full[2];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  uint64_t s_full[2], p_full[2], o_full[2];
+  // Of a tile of rows and a buffer of scores.  A waiter tells a phase from the one before it, and
+  // not from the one before that, so each buffer has barriers of its own: a step's scores come
+  // after the product of the step before the last, and its weights are waited for before the
+  // scores after the next.
+  uint64_t s_full[2][2], p_full[2][2], o_full[2][2];
   uint64_t drained;
   Item items[kItemRing];
   float4 scales[kScaleRing][kGroups];   // of 16 tokens: keys', log2 of values', 1 / values'
@@ -201,9 +210,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       mbar_init(&sh.k_empty[i], 1);
       mbar_init(&sh.v_full[i], kLoadThreads);
       mbar_init(&sh.v_empty[i], 1);
-      mbar_init(&sh.s_full[i], 2);
-      mbar_init(&sh.p_full[i], kTileRows);
-      mbar_init(&sh.o_full[i], 1);
+      for (int j = 0; j < 2; ++j) {
+        mbar_init(&sh.s_full[i][j], 2);
+        mbar_init(&sh.p_full[i][j], kTileRows);
+        mbar_init(&sh.o_full[i][j], 1);
+      }
     }
     mbar_init(&sh.drained, 1);
     fence_mbar_init();
@@ -284,15 +295,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         it.r = r;
         it.h = x % p.H;
         it.rows0 = max(pairs - 1 - x / p.H, 0) * kPairRows;
-        const int32_t i0 = it.rows0 / p.G, i1 = min(it.n - 1, (it.rows0 + kPairRows - 1) / p.G);
-        const int32_t see = p.causal ? min(it.len, it.len - it.n + i1 + 1) : it.len;
-        const int32_t from = p.window > 0 ? max(0, it.len - it.n + i0 - p.window + 1) : 0;
-        it.tile0 = from / kTileTokens;
-        it.tiles = (see + kTileTokens - 1) / kTileTokens - it.tile0;
-        if (it.tiles < 1) {                         // nothing is seen: one tile, hidden
-          it.tile0 = 0;
-          it.tiles = 1;
-        }
+        const int32_t before_q = it.len - it.n;     // the first query's position
+        if (p.window > 0)
+          it.tile0 = max(0, before_q + it.rows0 / p.G - p.window + 1) / kTileTokens;
+        const auto steps = [&](int32_t first) {     // of the tile of rows that begins there
+          if (first >= it.rows) return 0;
+          const int32_t i1 = min(it.n - 1, (first + kTileRows - 1) / p.G);
+          const int32_t see = p.causal ? min(it.len, before_q + i1 + 1) : it.len;
+          // (where nothing is seen: one, hidden)
+          return max(1, (see - it.tile0 * kTileTokens + kStepTokens - 1) / kStepTokens);
+        };
+        it.steps0 = steps(it.rows0);
+        it.steps1 = steps(it.rows0 + kTileRows);
+        it.tiles = (max(it.steps0, it.steps1) + 1) / 2;
         at += gridDim.x;
       }
       const uint32_t slot = items & (kItemRing - 1);
@@ -407,78 +422,76 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
   } else if (warp == kMmaWarp) {
     // ================================ products
     if (lane == 0) {
-      constexpr uint32_t id_qk = idesc_f16(kTileRows, kTileTokens, false);
+      constexpr uint32_t id_qk = idesc_f16(kTileRows, kStepTokens, false);
       constexpr uint32_t id_pv = idesc_f16(kTileRows, D, true);
       const uint64_t d_q = smem_desc_k_sw128(base + L::kQ);
       const uint64_t d_k = smem_desc_k_sw128(base + L::kK);
       const uint64_t d_v = smem_desc_mn_sw128(base + L::kV, L::kBlockBytes);
-      uint32_t tiles = 0, np[2] = {0, 0}, nq1 = 0;
-      const auto qk = [&](int x, uint32_t st) {
-        const uint64_t a = d_q + (x * L::kTileBytes >> 4), b = d_k + (st * L::kTileBytes >> 4);
+      constexpr uint32_t kHalf = kStepTokens * 128;   // bytes of a step's rows of K or V
+      const auto qk = [&](int x, uint32_t buf, uint32_t st, uint32_t half) {
+        const uint64_t a = d_q + (x * L::kTileBytes >> 4);
+        const uint64_t b = d_k + ((st * L::kTileBytes + half * kHalf) >> 4);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          constexpr int kPerBlock = 4;
-          const int off = ((k / kPerBlock) * L::kBlockBytes + (k % kPerBlock) * 32) >> 4;
-          umma_ss(tmem + x * kTileTokens, a + off, b + off, id_qk, k > 0);
+          const int off = ((k >> 2) * L::kBlockBytes + (k & 3) * 32) >> 4;
+          umma_ss(tmem + x * 2 * kStepTokens + buf * kStepTokens, a + off, b + off, id_qk, k > 0);
         }
+        umma_commit(&sh.s_full[x][buf]);
+        mbar_arrive(&sh.s_full[x][buf]);              // passes on what this thread has seen: the scales
       };
-      const auto pv = [&](int x, uint32_t st, bool add) {
-        const uint64_t b = d_v + (st * L::kTileBytes >> 4);
+      const auto pv = [&](int x, uint32_t buf, uint32_t st, uint32_t half, bool add) {
+        const uint64_t b = d_v + ((st * L::kTileBytes + half * kHalf) >> 4);
 #pragma unroll
-        for (int k = 0; k < kTileTokens / 16; ++k)
-          umma_ts(tmem + 2 * kTileTokens + x * D, tmem + x * kTileTokens + k * 8,
-                  b + (k * 2048 >> 4), id_pv, add || k > 0);
+        for (int k = 0; k < kStepTokens / 16; ++k)
+          umma_ts(tmem + 4 * kStepTokens + x * D,
+                  tmem + x * 2 * kStepTokens + buf * kStepTokens + k * 8, b + (k * 2048 >> 4),
+                  id_pv, add || k > 0);
+        umma_commit(&sh.o_full[x][buf]);
       };
-      // The arrival of this thread's own passes on what it has seen: the block scales.
-      const auto scored = [&](int x) {
-        umma_commit(&sh.s_full[x]);
-        mbar_arrive(&sh.s_full[x]);
-      };
+      uint32_t tiles = 0, ns[2] = {0, 0}, nq1 = 0;    // of the CTA; steps of each tile of rows
       bool ok = true;
       for (uint32_t items = 0; ok; ++items) {
         const uint32_t slot = items & (kItemRing - 1);
         if (!(ok = wait_one(&sh.item_full[slot], items / kItemRing))) break;
-        const int32_t n_tiles = sh.items[slot].tiles;
-        const bool two = sh.items[slot].rows - sh.items[slot].rows0 > kTileRows;
+        const int32_t s0 = sh.items[slot].steps0, s1 = sh.items[slot].steps1;
+        const int32_t steps = max(s0, s1);
         if (!sh.items[slot].more) break;
         mbar_arrive(&sh.item_empty[slot]);
         if (!(ok = wait_one(&sh.q_full[0], items))) break;
-        for (int32_t t = 0; t < n_tiles; ++t, ++tiles) {
-          const uint32_t st = tiles & 1, use = tiles >> 1;
-          if (!(ok = wait_one(&sh.k_full[st], use))) break;
-          tc_fence_after();
-          qk(0, st);
-          scored(0);
-          if (two) {
-            if (t > 0) {
-              if (!(ok = wait_one(&sh.p_full[1], np[1]++))) break;
-              tc_fence_after();
-              pv(1, st ^ 1, t > 1);
-              umma_commit(&sh.o_full[1]);
-              umma_commit(&sh.v_empty[st ^ 1]);
-            } else {
-              if (!(ok = wait_one(&sh.q_full[1], nq1++))) break;
+        if (s1 > 0 && !(ok = wait_one(&sh.q_full[1], nq1++))) break;
+        if (!(ok = wait_one(&sh.k_full[tiles & 1], tiles >> 1))) break;
+        tc_fence_after();
+        qk(0, ns[0] & 1, tiles & 1, 0);
+        if (s1 > 0) qk(1, ns[1] & 1, tiles & 1, 0);
+        if (steps == 1) umma_commit(&sh.k_empty[tiles & 1]);
+        for (int32_t u = 0; u < steps; ++u) {
+          if (u + 1 < steps) {                        // the next step's scores
+            const uint32_t half = (u + 1) & 1, tile = tiles + (half ? 0 : 1);
+            if (!half) {
+              if (!(ok = wait_one(&sh.k_full[tile & 1], tile >> 1))) break;
               tc_fence_after();
             }
-            qk(1, st);
-            scored(1);
+            if (u + 1 < s0) qk(0, (ns[0] + 1) & 1, tile & 1, half);
+            if (u + 1 < s1) qk(1, (ns[1] + 1) & 1, tile & 1, half);
+            if (half || u + 2 == steps) umma_commit(&sh.k_empty[tile & 1]);
           }
-          umma_commit(&sh.k_empty[st]);
-          if (!(ok = wait_one(&sh.v_full[st], use))) break;
-          if (!(ok = wait_one(&sh.p_full[0], np[0]++))) break;
-          tc_fence_after();
-          pv(0, st, t > 0);
-          umma_commit(&sh.o_full[0]);
-          if (!two) umma_commit(&sh.v_empty[st]);
-        }
-        if (!ok) break;
-        if (two) {
-          const uint32_t st = (tiles - 1) & 1;
-          if (!(ok = wait_one(&sh.p_full[1], np[1]++))) break;
-          tc_fence_after();
-          pv(1, st, n_tiles > 1);
-          umma_commit(&sh.o_full[1]);
-          umma_commit(&sh.v_empty[st]);
+          if (!(u & 1) && !(ok = wait_one(&sh.v_full[tiles & 1], tiles >> 1))) break;
+          if (u < s0) {
+            if (!(ok = wait_one(&sh.p_full[0][ns[0] & 1], ns[0] >> 1))) break;
+            tc_fence_after();
+            pv(0, ns[0] & 1, tiles & 1, u & 1, u > 0);
+            ++ns[0];
+          }
+          if (u < s1) {
+            if (!(ok = wait_one(&sh.p_full[1][ns[1] & 1], ns[1] >> 1))) break;
+            tc_fence_after();
+            pv(1, ns[1] & 1, tiles & 1, u & 1, u > 0);
+            ++ns[1];
+          }
+          if ((u & 1) || u + 1 == steps) {
+            umma_commit(&sh.v_empty[tiles & 1]);
+            ++tiles;
+          }
         }
       }
       umma_commit(&sh.drained);                     // nothing of it runs on when memory is given back
@@ -494,69 +507,93 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     const int x = warp >> 2;                        // which tile of rows
     const int row = (warp & 3) * 32 + lane;         // of it, and lane of tensor memory
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + lanes + x * kTileTokens;
-    const uint32_t t_o = tmem + lanes + 2 * kTileTokens + x * D;
-    const uint32_t q_line = base + L::kQ + x * L::kTileBytes + row * 128;
-    uint32_t items = 0, tiles = 0, ns = 0;          // of the CTA; of this group
+    const uint32_t t_s = tmem + lanes + x * 2 * kStepTokens;
+    const uint32_t t_o = tmem + lanes + 4 * kStepTokens + x * D;
+    uint32_t items = 0, tiles = 0, ns = 0;          // of the CTA; steps of this tile of rows
     bool ok = true;
 
-    // The next item that has rows of this group's, and this thread's row of its queries.  Its
-    // place in shared memory is free: the group's last scores are there.
-    Item it{};
-    int32_t rows0 = 0, qi = 0, qj = 0;
-    float qs = 0.0f;
-    const auto take = [&]() {
+    // Queries: D / 8 lanes a row, 8 values each, so that a load is of whole rows.
+    constexpr int LR = D / 8, RS = 32 / LR, NQ = 32 / RS;  // lanes of a row, rows of a load, loads
+    Item it{}, next{};
+    uint4 qv[NQ / 2];                               // half of them at a time
+    const auto output_row = [&](const Item& w, int32_t full) {
+      const int32_t i = full / p.G, j = full - i * p.G;
+      return (int64_t)(w.q0 + i) * (p.H * p.G) + w.h * p.G + j;
+    };
+    // The next item with rows of this tile's, if it has been said: the items up to it may have to
+    // be done first, and they may need the step that this tile of rows is at.
+    const auto take = [&](bool block) {
       for (;;) {
-        const uint32_t slot = items & (kItemRing - 1);
-        if (!(ok = wait(&sh.item_full[slot], items / kItemRing))) return;
-        it = sh.items[slot];
+        const uint32_t slot = items & (kItemRing - 1), phase = items / kItemRing;
+        if (block) {
+          if (!(ok = wait(&sh.item_full[slot], phase))) return false;
+        } else if (!__all_sync(0xffffffffu,
+                               mbar_try_wait(smem_u32(&sh.item_full[slot]), phase & 1u))) {
+          return false;
+        }
+        next = sh.items[slot];
         __syncwarp();
-        if (!it.more) return;
+        if (!next.more) return true;
         if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
         ++items;
-        rows0 = it.rows0 + x * kTileRows;
-        if (rows0 < it.rows) break;
-        tiles += it.tiles;
+        if ((x ? next.steps1 : next.steps0) > 0) return true;
+        tiles += next.tiles;
       }
-      const int32_t full = min(rows0 + row, it.rows - 1);
-      qi = full / p.G;
-      qj = full - qi * p.G;
-      const uint16_t* src = p.q + (int64_t)(it.q0 + qi) * p.q_token +
-                            (int64_t)(it.h * p.G + qj) * p.q_head;
-      uint4 v[D / 8];
-      if (p.q_vec) {
+    };
+    const auto fetch = [&](int i0) {                // its queries, on their way
 #pragma unroll
-        for (int c = 0; c < D / 8; ++c) v[c] = __ldg(reinterpret_cast<const uint4*>(src) + c);
-      } else {
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) v[c] = attend_raw8(src + c * 8);
+      for (int i = 0; i < NQ / 2; ++i) {
+        const int32_t full =
+            next.rows0 + x * kTileRows + (warp & 3) * 32 + (i0 + i) * RS + lane / LR;
+        qv[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (next.more && full < next.rows) {
+          const int32_t a = full / p.G, b = full - a * p.G;
+          const uint16_t* src = p.q + (int64_t)(next.q0 + a) * p.q_token +
+                                (int64_t)(next.h * p.G + b) * p.q_head + (lane % LR) * 8;
+          qv[i] = p.q_vec ? __ldg(reinterpret_cast<const uint4*>(src)) : attend_raw8(src);
+        }
       }
-      float big = 0.0f;
+    };
+    float qs = 0.0f, qs_next = 0.0f;
+    const auto put = [&](int i0) {                  // and into place: the last scores are there
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        float f[8];
-        attend_unpack8(v[c], p.fp16, f);
+      for (int i = 0; i < NQ / 2; ++i) {
+        float f[8], big = 0.0f;
+        attend_unpack8(qv[i], p.fp16, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(f[e]));
-      }
-      // a power of two of the row's size, kept where it and its inverse are normal
-      const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
-      const float by = __uint_as_float((254u - e) << 23);
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        float f[8];
-        attend_unpack8(v[c], p.fp16, f);
-        sts128(q_line + (c >> 3) * L::kBlockBytes + (((c ^ row) & 7) << 4),
+        for (int o = 1; o < LR; o <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+        // a power of two of the row's size, kept where it and its inverse are normal
+        const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+        const float by = __uint_as_float((254u - e) << 23);
+        const int r = (warp & 3) * 32 + (i0 + i) * RS + lane / LR, ch = lane % LR;
+        sts128(base + L::kQ + x * L::kTileBytes + (ch >> 3) * L::kBlockBytes + r * 128 +
+                   (((ch ^ r) & 7) << 4),
                half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
                half2_of(f[4] * by, f[5] * by), half2_of(f[6] * by, f[7] * by));
+        const uint32_t mine = __shfl_sync(0xffffffffu, e, (lane % RS) * LR);
+        if (lane / RS == i0 + i) qs_next = __uint_as_float(mine << 23) * p.scale_log2;
       }
-      qs = __uint_as_float(e << 23) * p.scale_log2;
+    };
+    const auto put_all = [&]() {                    // the first half was fetched
+      put(0);
+      fetch(NQ / 2);
+      put(NQ / 2);
       fence_async_shared();
       mbar_arrive(&sh.q_full[x]);
     };
-    take();
-    while (ok && it.more) {
-      const int32_t n_tiles = it.tiles, pos = it.len - it.n + qi;
+    bool known = take(true);
+    if (ok && next.more) {
+      fetch(0);
+      put_all();
+    }
+    while (ok && next.more) {
+      it = next;
+      qs = qs_next;
+      const int32_t n_steps = x ? it.steps1 : it.steps0;
+      const int32_t rows0 = it.rows0 + x * kTileRows;
+      const int32_t pos = it.len - it.n + min(rows0 + row, it.rows - 1) / p.G;
       const int32_t top = p.causal ? min(pos, it.len - 1) : it.len - 1;
       const int32_t bottom = p.window > 0 ? pos - p.window + 1 : 0;
       // tokens that every row of the tile sees: from .. to
@@ -564,42 +601,57 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       const int32_t pos1 = it.len - it.n + min(it.n - 1, (rows0 + kTileRows - 1) / p.G);
       const int32_t to = p.causal ? min(pos0, it.len - 1) : it.len - 1;
       const int32_t from = p.window > 0 ? pos1 - p.window + 1 : 0;
+      const uint32_t tile_base = tiles;
+      tiles += it.tiles;
 
       float m = -INFINITY, sum = 0.0f;
-      for (int32_t t = 0; t < n_tiles; ++t, ++tiles, ++ns) {
-        if (!(ok = wait(&sh.s_full[x], ns))) break;
+      for (int32_t u = 0; u < n_steps; ++u, ++ns) {
+        const uint32_t buf = ns & 1;
+        if (u + 1 == n_steps) {                     // what follows, on its way
+          known = take(false);
+          if (known) fetch(0);
+        }
+        if (!(ok = wait(&sh.s_full[x][buf], ns >> 1))) break;
         tc_fence_after();
-        const float4* scales = sh.scales[tiles & (kScaleRing - 1)];
-        const int32_t t0 = (it.tile0 + t) * kTileTokens;
-        uint32_t a[kTileTokens];
+        const float4* scales =
+            sh.scales[(tile_base + (u >> 1)) & (kScaleRing - 1)] + (u & 1) * kStepGroups;
+        const int32_t t0 = it.tile0 * kTileTokens + u * kStepTokens;
+        uint32_t a[kStepTokens];
+        tmem_ld_32x32b_x32(t_s + buf * kStepTokens, *reinterpret_cast<uint32_t(*)[32]>(a));
+        tmem_ld_32x32b_x32(t_s + buf * kStepTokens + 32, *reinterpret_cast<uint32_t(*)[32]>(a + 32));
+        float by[kStepGroups], lv[kStepGroups];
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-          tmem_ld_32x32b_x32(t_s + c * 32, *reinterpret_cast<uint32_t(*)[32]>(a + c * 32));
+        for (int g = 0; g < kStepGroups; ++g) {
+          by[g] = factor(scales[g].x, qs);
+          lv[g] = scales[g].y;
+        }
         tmem_ld_wait();
-        if (t0 < from || t0 + kTileTokens - 1 > to) {
+        if (t0 < from || t0 + kStepTokens - 1 > to) {
           const int32_t last = top - t0, first = bottom - t0;
 #pragma unroll
-          for (int e = 0; e < kTileTokens; ++e)
+          for (int e = 0; e < kStepTokens; ++e)
             if (e > last || e < first) a[e] = 0xff800000u;  // -inf
         }
         // ---- the maximum of acc * c + lv
+        float b[kStepGroups];
+#pragma unroll
+        for (int g = 0; g < kStepGroups; ++g) b[g] = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; e += 2)
+#pragma unroll
+          for (int g = 0; g < kStepGroups; ++g)
+            b[g] = fmaxf(b[g], fmaxf(__uint_as_float(a[g * 16 + e]),
+                                     __uint_as_float(a[g * 16 + e + 1])));
         float most = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          float b = -INFINITY;
-#pragma unroll
-          for (int e = 0; e < 16; ++e) b = fmaxf(b, __uint_as_float(a[g * 16 + e]));
-          const float4 sc = scales[g];
-          most = fmaxf(most, fmaf(b, factor(sc.x, qs), sc.y));
-        }
-        const bool grow = most > m + kTilesLag;
-        if (__any_sync(0xffffffffu, grow)) {
+        for (int g = 0; g < kStepGroups; ++g) most = fmaxf(most, fmaf(b[g], by[g], lv[g]));
+        if (__any_sync(0xffffffffu, most > m + kTilesLag)) {
           const float now = fmaxf(m, most);
           const float f = m == -INFINITY ? 0.0f : fast_exp2(m - now);
           m = now;
           sum *= f;
-          if (t > 0) {
-            if (!(ok = wait(&sh.o_full[x], ns - 1))) break;
+          if (u > 0) {
+            if (!(ok = wait(&sh.o_full[x][(ns - 1) & 1], (ns - 1) >> 1))) break;
             tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
@@ -614,70 +666,88 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         }
         // ---- the weights
         const float shift = m == -INFINITY ? 0.0f : kTilesShift - m;
+        uint64_t part[kStepGroups];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int g = 0; g < kStepGroups; ++g) part[g] = 0;
+#pragma unroll
+        for (int c = 0; c < kStepGroups / 2; ++c) {
           uint32_t w[16];
 #pragma unroll
-          for (int g = 0; g < 2; ++g) {
-            const float4 sc = scales[c * 2 + g];
-            const float by = factor(sc.x, qs), add = sc.y + shift;
-            const uint64_t by2 = pack_f32x2(by, by), add2 = pack_f32x2(add, add);
-            uint64_t part = 0;
+          for (int y = 0; y < 2; ++y) {
+            const int g = c * 2 + y;
+            const float add = lv[g] + shift;
+            const uint64_t by2 = pack_f32x2(by[g], by[g]), add2 = pack_f32x2(add, add);
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-              const int k = c * 32 + g * 16 + e;
+              const int k = g * 16 + e;
               float z0, z1;
               unpack_f32x2(fma_f32x2(pack_b32x2(a[k], a[k + 1]), by2, add2), z0, z1);
               z0 = fast_exp2(z0);
               z1 = fast_exp2(z1);
-              part = add_f32x2(part, pack_f32x2(z0, z1));
-              w[g * 8 + e / 2] = half2_of(z0, z1);
+              part[g] = add_f32x2(part[g], pack_f32x2(z0, z1));
+              w[y * 8 + e / 2] = half2_of(z0, z1);
             }
-            float p0, p1;
-            unpack_f32x2(part, p0, p1);
-            sum = fmaf(p0 + p1, sc.z, sum);
           }
-          tmem_st_32x32b_x16(t_s + c * 16, w);
+          tmem_st_32x32b_x16(t_s + buf * kStepTokens + c * 16, w);
+        }
+#pragma unroll
+        for (int g = 0; g < kStepGroups; ++g) {
+          float p0, p1;
+          unpack_f32x2(part[g], p0, p1);
+          sum = fmaf(p0 + p1, scales[g].z, sum);
         }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&sh.p_full[x]);
+        mbar_arrive(&sh.p_full[x][buf]);            // (the scales' place may be written from here on)
       }
       if (!ok) break;
 
       // ---- the output, after the next item's queries
-      const bool mine = rows0 + row < it.rows;
-      const int64_t out_row = (int64_t)(it.q0 + qi) * (p.H * p.G) + it.h * p.G + qj;
+      if (known && next.more) put_all();
       const bool none = sum == 0.0f;
       const float inv = none ? 0.0f : __fdividef(1.0f, sum);
-      const uint32_t last = ns - 1;
-      take();
-      if (!ok || !(ok = wait(&sh.o_full[x], last))) break;
+      if (p.lse && rows0 + row < it.rows)
+        p.lse[output_row(it, rows0 + row)] =
+            none ? -INFINITY : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
+      if (!(ok = wait(&sh.o_full[x][(ns - 1) & 1], (ns - 1) >> 1))) break;
       tc_fence_after();
+      // 32 of dim at a time through shared memory: a thread has a row, a store 64 bytes of eight
+      const uint32_t stage = base + L::kOut + warp * 2048;
+      uint16_t* dst[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int32_t full = rows0 + (warp & 3) * 32 + v * 8 + (lane >> 2);
+        dst[v] = full < it.rows ? p.out + output_row(it, full) * D + (lane & 3) * 8 : nullptr;
+      }
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         uint32_t o[32];
         tmem_ld_32x32b_x32(t_o + c * 32, o);
         tmem_ld_wait();
-        if (mine) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + out_row * D + c * 32);
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            uint32_t w[4];
+        for (int v = 0; v < 4; ++v) {
+          uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float lo = __uint_as_float(o[v * 8 + 2 * e]) * inv;
-              const float hi = __uint_as_float(o[v * 8 + 2 * e + 1]) * inv;
-              w[e] = none ? 0u : attend_pack2(p.fp16, lo, hi);
-            }
-            dst[v] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
+          for (int e = 0; e < 4; ++e)
+            w[e] = none ? 0u
+                        : attend_pack2(p.fp16, __uint_as_float(o[v * 8 + 2 * e]) * inv,
+                                       __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
+          sts128(stage + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
         }
+        __syncwarp();
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int r = v * 8 + (lane >> 2);
+          const uint4 y = lds128(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+          if (dst[v]) *reinterpret_cast<uint4*>(dst[v] + c * 32) = y;
+        }
+        __syncwarp();
       }
-      if (mine && p.lse)
-        p.lse[out_row] = none ? -INFINITY
-                              : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
       tc_fence_before();
+      if (!known && take(true) && next.more) {
+        fetch(0);
+        put_all();
+      }
     }
   }
   tc_fence_before();
