@@ -134,6 +134,17 @@ __device__ __forceinline__ uint64_t smem_desc_mn_sw128(uint32_t saddr, uint32_t 
   return d;
 }
 
+// One thread of a converged warp, the same each time.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(p));
+  return p != 0;
+}
+
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -257,9 +268,6 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
   const int32_t total = sh.before[kTilesThreads];
   const uint32_t tmem = sh.tmem;
   volatile int* abort = &sh.abort;
-  const auto wait_one = [&](uint64_t* bar, uint32_t phase) {
-    return mbar_wait(bar, phase & 1u, abort);
-  };
   const auto wait = [&](uint64_t* bar, uint32_t phase) {  // a warp goes on, or gives up, as one
     return __all_sync(0xffffffffu, mbar_wait(bar, phase & 1u, abort)) != 0;
   };
@@ -421,7 +429,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     }
   } else if (warp == kMmaWarp) {
     // ================================ products
-    if (lane == 0) {
+    // The whole warp runs this, so that descriptors stay in uniform registers; one thread issues.
+    {
       constexpr uint32_t id_qk = idesc_f16(kTileRows, kStepTokens, false);
       constexpr uint32_t id_pv = idesc_f16(kTileRows, D, true);
       const uint64_t d_q = smem_desc_k_sw128(base + L::kQ);
@@ -431,70 +440,83 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       const auto qk = [&](int x, uint32_t buf, uint32_t st, uint32_t half) {
         const uint64_t a = d_q + (x * L::kTileBytes >> 4);
         const uint64_t b = d_k + ((st * L::kTileBytes + half * kHalf) >> 4);
+        const uint32_t to = tmem + x * 2 * kStepTokens + buf * kStepTokens;
+        if (elect_one()) {
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const int off = ((k >> 2) * L::kBlockBytes + (k & 3) * 32) >> 4;
-          umma_ss(tmem + x * 2 * kStepTokens + buf * kStepTokens, a + off, b + off, id_qk, k > 0);
+          for (int k = 0; k < D / 16; ++k) {
+            const int off = ((k >> 2) * L::kBlockBytes + (k & 3) * 32) >> 4;
+            umma_ss(to, a + off, b + off, id_qk, k > 0);
+          }
+          umma_commit(&sh.s_full[x][buf]);
+          mbar_arrive(&sh.s_full[x][buf]);            // passes on what this thread has seen: the scales
         }
-        umma_commit(&sh.s_full[x][buf]);
-        mbar_arrive(&sh.s_full[x][buf]);              // passes on what this thread has seen: the scales
+        __syncwarp();
       };
       const auto pv = [&](int x, uint32_t buf, uint32_t st, uint32_t half, bool add) {
         const uint64_t b = d_v + ((st * L::kTileBytes + half * kHalf) >> 4);
+        const uint32_t to = tmem + 4 * kStepTokens + x * D;
+        const uint32_t from = tmem + x * 2 * kStepTokens + buf * kStepTokens;
+        if (elect_one()) {
+          umma_ts(to, from, b, id_pv, add);
 #pragma unroll
-        for (int k = 0; k < kStepTokens / 16; ++k)
-          umma_ts(tmem + 4 * kStepTokens + x * D,
-                  tmem + x * 2 * kStepTokens + buf * kStepTokens + k * 8, b + (k * 2048 >> 4),
-                  id_pv, add || k > 0);
-        umma_commit(&sh.o_full[x][buf]);
+          for (int k = 1; k < kStepTokens / 16; ++k)
+            umma_ts(to, from + k * 8, b + (k * 2048 >> 4), id_pv, 1);
+          umma_commit(&sh.o_full[x][buf]);
+        }
+        __syncwarp();
+      };
+      const auto commit = [&](uint64_t* bar) {
+        if (elect_one()) umma_commit(bar);
+        __syncwarp();
       };
       uint32_t tiles = 0, ns[2] = {0, 0}, nq1 = 0;    // of the CTA; steps of each tile of rows
       bool ok = true;
       for (uint32_t items = 0; ok; ++items) {
         const uint32_t slot = items & (kItemRing - 1);
-        if (!(ok = wait_one(&sh.item_full[slot], items / kItemRing))) break;
+        if (!(ok = wait(&sh.item_full[slot], items / kItemRing))) break;
         const int32_t s0 = sh.items[slot].steps0, s1 = sh.items[slot].steps1;
         const int32_t steps = max(s0, s1);
         if (!sh.items[slot].more) break;
-        mbar_arrive(&sh.item_empty[slot]);
-        if (!(ok = wait_one(&sh.q_full[0], items))) break;
-        if (s1 > 0 && !(ok = wait_one(&sh.q_full[1], nq1++))) break;
-        if (!(ok = wait_one(&sh.k_full[tiles & 1], tiles >> 1))) break;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
+        if (!(ok = wait(&sh.q_full[0], items))) break;
+        if (s1 > 0 && !(ok = wait(&sh.q_full[1], nq1++))) break;
+        if (!(ok = wait(&sh.k_full[tiles & 1], tiles >> 1))) break;
         tc_fence_after();
         qk(0, ns[0] & 1, tiles & 1, 0);
         if (s1 > 0) qk(1, ns[1] & 1, tiles & 1, 0);
-        if (steps == 1) umma_commit(&sh.k_empty[tiles & 1]);
+        if (steps == 1) commit(&sh.k_empty[tiles & 1]);
         for (int32_t u = 0; u < steps; ++u) {
           if (u + 1 < steps) {                        // the next step's scores
             const uint32_t half = (u + 1) & 1, tile = tiles + (half ? 0 : 1);
             if (!half) {
-              if (!(ok = wait_one(&sh.k_full[tile & 1], tile >> 1))) break;
+              if (!(ok = wait(&sh.k_full[tile & 1], tile >> 1))) break;
               tc_fence_after();
             }
             if (u + 1 < s0) qk(0, (ns[0] + 1) & 1, tile & 1, half);
             if (u + 1 < s1) qk(1, (ns[1] + 1) & 1, tile & 1, half);
-            if (half || u + 2 == steps) umma_commit(&sh.k_empty[tile & 1]);
+            if (half || u + 2 == steps) commit(&sh.k_empty[tile & 1]);
           }
-          if (!(u & 1) && !(ok = wait_one(&sh.v_full[tiles & 1], tiles >> 1))) break;
+          if (!(u & 1) && !(ok = wait(&sh.v_full[tiles & 1], tiles >> 1))) break;
           if (u < s0) {
-            if (!(ok = wait_one(&sh.p_full[0][ns[0] & 1], ns[0] >> 1))) break;
+            if (!(ok = wait(&sh.p_full[0][ns[0] & 1], ns[0] >> 1))) break;
             tc_fence_after();
             pv(0, ns[0] & 1, tiles & 1, u & 1, u > 0);
             ++ns[0];
           }
           if (u < s1) {
-            if (!(ok = wait_one(&sh.p_full[1][ns[1] & 1], ns[1] >> 1))) break;
+            if (!(ok = wait(&sh.p_full[1][ns[1] & 1], ns[1] >> 1))) break;
             tc_fence_after();
             pv(1, ns[1] & 1, tiles & 1, u & 1, u > 0);
             ++ns[1];
           }
           if ((u & 1) || u + 1 == steps) {
-            umma_commit(&sh.v_empty[tiles & 1]);
+            commit(&sh.v_empty[tiles & 1]);
             ++tiles;
           }
         }
       }
-      umma_commit(&sh.drained);                     // nothing of it runs on when memory is given back
+      commit(&sh.drained);                     // nothing of it runs on when memory is given back
       if (!mbar_wait_limit(&sh.drained, 0, abort, kWaitLimitNs)) {
         const uint64_t t0 = globaltimer_ns();       // someone gave up: wait for what was issued
         while (!mbar_try_wait(smem_u32(&sh.drained), 0) && globaltimer_ns() - t0 < kWaitLimitNs) {
