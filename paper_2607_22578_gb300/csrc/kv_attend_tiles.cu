@@ -1,19 +1,20 @@
 // Attention of many query rows over the paged 8-bit cache (hs_kv_attend): prompts, chunks and
 // cross attention, on the tensor cores.
 //
-// The formula is kv_attend.cu's.  A step is 128 rows (query, head of the group) against 64 tokens:
-// s = q k^T is one tcgen05.mma per 16 of dim (M = 128, N = 64) into tensor memory, o += p v one per
-// 16 tokens (N = dim) with p as its A operand in tensor memory.  4 flops a (row, token, dim) and one
-// exponential a (row, token): tensor cores and exponentials bound it together, so a CTA keeps two
-// tiles of rows going and each has two buffers of scores: the next step's are there when a step's
-// weights are done (with one buffer, of 128 tokens, a tile of rows waits for both products: 5500
-// clocks for 128 tokens, of which the products are 2300).
+// The formula is kv_attend.cu's.  A step is 128 rows (query, head of the group) against 128
+// tokens: s = q k^T is one tcgen05.mma per 16 of dim (M = 128, N = 128) into tensor memory, o += p v
+// one per 16 tokens (N = dim) with p as its A operand in tensor memory, where the scores were.  4
+// flops a (row, token, dim) and one exponential a (row, token): tensor cores and exponentials bound
+// it together, so a CTA keeps two tiles of rows in flight that take turns: while one's scores become
+// weights, the tensor cores work for the other.  Scores become weights by halves of the tokens, each
+// a step of the running maximum, and each half is handed over when it is done.
+// (Two buffers of scores of 64 tokens each instead of one of 128: a product of N = 64 takes as long
+// as one of 128, 75 clocks, and the whole 4700 clocks for 128 tokens.)
 //
 //   warps 0-3, 4-7   a thread a row: its query into shared memory, scores to weights, the output
-//   warps 8-10       codes from the cache's blocks, decoded to half in shared memory (swizzled;
+//   warps 8-14       codes from the cache's blocks, decoded to half in shared memory (swizzled;
 //                    K and V alike: K is read along dim, V across it), a tile ahead in registers
-//   warp 11          one thread issues every product
-// Twelve warps, so that a thread may have 168 registers: a row's 128 scores stay in them.
+//   warp 15          one thread issues every product
 //
 // CTAs are persistent, one an SM.  Work is (request, pair of tiles of rows, kv head) items, the
 // later pairs of a request (which see more) first; an item's queries and first tokens are loaded
@@ -34,13 +35,13 @@ constexpr int kTileRows = 128;
 constexpr int kPairRows = 2 * kTileRows;
 constexpr int kTileTokens = 128;
 constexpr int kGroups = kTileTokens / 16;      // 16 tokens lie in one block: one scale
-constexpr int kStepTokens = 64;                // of scores that are computed at once
-constexpr int kStepGroups = kStepTokens / 16;
 constexpr int kSoftWarps = 8;
-constexpr int kLoadWarp = 8;                   // the first of three
-constexpr int kLoadWarps = 3;
-constexpr int kMmaWarp = 11;
-constexpr int kTilesThreads = 12 * 32;
+constexpr int kLoadWarp = 8;                   // the first of seven
+constexpr int kLoadWarps = 7;
+constexpr int kMmaWarp = 15;
+constexpr int kTilesThreads = 16 * 32;
+constexpr int kHalfTokens = kTileTokens / 2;
+constexpr int kHalfGroups = kGroups / 2;
 constexpr int kLoadThreads = kLoadWarps * 32;
 constexpr int kScaleRing = 4;                  // tiles
 constexpr int kItemRing = 4;
@@ -63,7 +64,7 @@ struct TilesLayout {
 struct Item {
   int32_t r, h, rows0, n, q0, len;
   int32_t tile0, tiles, rows;        // tiles of tokens; rows of the request
-  int32_t steps0, steps1;            // of 64 tokens, for each tile of rows (0: it has no rows)
+  int32_t steps0, steps1;            // of these for each tile of rows (0: it has no rows)
   int32_t more;                      // 0: no further item
 };
 
@@ -71,11 +72,8 @@ struct TilesShared {
   uint64_t item_full[kItemRing], item_empty[kItemRing];
   uint64_t q_full[2];
   uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
-  // Of a tile of rows and a buffer of scores.  A waiter tells a phase from the one before it, and
-  // not from the one before that, so each buffer has barriers of its own: a step's scores come
-  // after the product of the step before the last, and its weights are waited for before the
-  // scores after the next.
-  uint64_t s_full[2][2], p_full[2][2], o_full[2][2];
+  uint64_t s_full[2];                   // of a tile of rows
+  uint64_t p_full[2][2], o_full[2][2];  // ... and half of the tokens
   uint64_t drained;
   Item items[kItemRing];
   float4 scales[kScaleRing][kGroups];   // of 16 tokens: keys', log2 of values', 1 / values'
@@ -221,8 +219,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       mbar_init(&sh.k_empty[i], 1);
       mbar_init(&sh.v_full[i], kLoadThreads);
       mbar_init(&sh.v_empty[i], 1);
+      mbar_init(&sh.s_full[i], 2);
       for (int j = 0; j < 2; ++j) {
-        mbar_init(&sh.s_full[i][j], 2);
         mbar_init(&sh.p_full[i][j], kTileRows);
         mbar_init(&sh.o_full[i][j], 1);
       }
@@ -311,11 +309,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
           const int32_t i1 = min(it.n - 1, (first + kTileRows - 1) / p.G);
           const int32_t see = p.causal ? min(it.len, before_q + i1 + 1) : it.len;
           // (where nothing is seen: one, hidden)
-          return max(1, (see - it.tile0 * kTileTokens + kStepTokens - 1) / kStepTokens);
+          return max(1, (see + kTileTokens - 1) / kTileTokens - it.tile0);
         };
         it.steps0 = steps(it.rows0);
         it.steps1 = steps(it.rows0 + kTileRows);
-        it.tiles = (max(it.steps0, it.steps1) + 1) / 2;
+        it.tiles = max(it.steps0, it.steps1);
         at += gridDim.x;
       }
       const uint32_t slot = items & (kItemRing - 1);
@@ -345,23 +343,28 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         sid = t_0 + lane * 16 < t_len ? __ldg(row + ((t_0 + lane * 16) >> p.bt_log2)) : -1;
       if (++tile == it.tile0 + it.tiles) next_item();
     };
+    int64_t off[RG];                                // of this thread's 16 bytes; -1: no token
     uint4 kr[RG][CH], vr[RG][CH];
     float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const auto fetch = [&](const uint8_t* codes, uint4 (&to)[RG][CH]) {
+    const auto place = [&]() {
 #pragma unroll
       for (int i = 0; i < RG; ++i) {
         const int32_t tok = t_0 + (lw + i * kLoadWarps) * 8 + row8, id = ids[i];
         const bool known = (uint32_t)id < (uint32_t)p.n_blocks;
-        const bool in = tok < t_len && known;
         if (id != -1 && !known) bad = kErrInvalidArg;
-        const uint8_t* src =
-            codes + (((((int64_t)(in ? id : 0) * p.H + t_h) << p.bt_log2) +
-                      (tok & ((1 << p.bt_log2) - 1))) * D) + chunk * 16;
+        off[i] = known && tok < t_len
+                     ? ((((int64_t)id * p.H + t_h) << p.bt_log2) + (tok & ((1 << p.bt_log2) - 1))) * D +
+                           chunk * 16
+                     : -1;
+      }
+    };
+    const auto fetch = [&](const uint8_t* codes, uint4 (&to)[RG][CH]) {
+#pragma unroll
+      for (int i = 0; i < RG; ++i)
 #pragma unroll
         for (int c = 0; c < CH; ++c)
-          to[i][c] = in ? __ldg(reinterpret_cast<const uint4*>(src + c * 64))
-                        : make_uint4(0u, 0u, 0u, 0u);
-      }
+          to[i][c] = off[i] >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + off[i] + c * 64))
+                                 : make_uint4(0u, 0u, 0u, 0u);
     };
     const auto fetch_scale = [&]() {
       if (lw == 0 && lane < kGroups) {
@@ -397,6 +400,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     bool fetched = more && ok;
     if (fetched) {
       look_up();
+      place();
       fetch(p.k, kr);
       fetch(p.v, vr);
       fetch_scale();
@@ -415,6 +419,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       fence_async_shared();
       mbar_arrive(&sh.k_full[st]);
       if (looked) {
+        place();
         fetch(p.k, kr);
         fetch_scale();
       }
@@ -431,37 +436,35 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     // ================================ products
     // The whole warp runs this, so that descriptors stay in uniform registers; one thread issues.
     {
-      constexpr uint32_t id_qk = idesc_f16(kTileRows, kStepTokens, false);
+      constexpr uint32_t id_qk = idesc_f16(kTileRows, kTileTokens, false);
       constexpr uint32_t id_pv = idesc_f16(kTileRows, D, true);
       const uint64_t d_q = smem_desc_k_sw128(base + L::kQ);
       const uint64_t d_k = smem_desc_k_sw128(base + L::kK);
       const uint64_t d_v = smem_desc_mn_sw128(base + L::kV, L::kBlockBytes);
-      constexpr uint32_t kHalf = kStepTokens * 128;   // bytes of a step's rows of K or V
-      const auto qk = [&](int x, uint32_t buf, uint32_t st, uint32_t half) {
-        const uint64_t a = d_q + (x * L::kTileBytes >> 4);
-        const uint64_t b = d_k + ((st * L::kTileBytes + half * kHalf) >> 4);
-        const uint32_t to = tmem + x * 2 * kStepTokens + buf * kStepTokens;
+      const auto qk = [&](int x, uint32_t st) {
+        const uint64_t a = d_q + (x * L::kTileBytes >> 4), b = d_k + (st * L::kTileBytes >> 4);
+        const uint32_t to = tmem + x * kTileTokens;
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const int off = ((k >> 2) * L::kBlockBytes + (k & 3) * 32) >> 4;
             umma_ss(to, a + off, b + off, id_qk, k > 0);
           }
-          umma_commit(&sh.s_full[x][buf]);
-          mbar_arrive(&sh.s_full[x][buf]);            // passes on what this thread has seen: the scales
+          umma_commit(&sh.s_full[x]);
+          mbar_arrive(&sh.s_full[x]);                 // passes on what this thread has seen: the scales
         }
         __syncwarp();
       };
-      const auto pv = [&](int x, uint32_t buf, uint32_t st, uint32_t half, bool add) {
-        const uint64_t b = d_v + ((st * L::kTileBytes + half * kHalf) >> 4);
-        const uint32_t to = tmem + 4 * kStepTokens + x * D;
-        const uint32_t from = tmem + x * 2 * kStepTokens + buf * kStepTokens;
+      const auto pv = [&](int x, uint32_t st, int half, bool add) {
+        const uint64_t b = d_v + (st * L::kTileBytes >> 4);
+        const uint32_t to = tmem + 2 * kTileTokens + x * D, from = tmem + x * kTileTokens;
         if (elect_one()) {
-          umma_ts(to, from, b, id_pv, add);
 #pragma unroll
-          for (int k = 1; k < kStepTokens / 16; ++k)
-            umma_ts(to, from + k * 8, b + (k * 2048 >> 4), id_pv, 1);
-          umma_commit(&sh.o_full[x][buf]);
+          for (int i = 0; i < kTileTokens / 32; ++i) {
+            const int k = half * (kTileTokens / 32) + i;
+            umma_ts(to, from + k * 8, b + (k * 2048 >> 4), id_pv, k > 0 ? 1u : add);
+          }
+          umma_commit(&sh.o_full[x][half]);
         }
         __syncwarp();
       };
@@ -479,42 +482,42 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         if (!sh.items[slot].more) break;
         __syncwarp();
         if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
-        if (!(ok = wait(&sh.q_full[0], items))) break;
-        if (s1 > 0 && !(ok = wait(&sh.q_full[1], nq1++))) break;
-        if (!(ok = wait(&sh.k_full[tiles & 1], tiles >> 1))) break;
-        tc_fence_after();
-        qk(0, ns[0] & 1, tiles & 1, 0);
-        if (s1 > 0) qk(1, ns[1] & 1, tiles & 1, 0);
-        if (steps == 1) commit(&sh.k_empty[tiles & 1]);
-        for (int32_t u = 0; u < steps; ++u) {
-          if (u + 1 < steps) {                        // the next step's scores
-            const uint32_t half = (u + 1) & 1, tile = tiles + (half ? 0 : 1);
-            if (!half) {
-              if (!(ok = wait(&sh.k_full[tile & 1], tile >> 1))) break;
-              tc_fence_after();
+        // Step u's scores come after step u - 1's output, which read weights from their place.
+        for (int32_t u = 0; u <= steps && ok; ++u) {
+          const uint32_t tile = tiles + u, st = tile & 1;
+          if (u < steps) {
+            if (!(ok = wait(&sh.k_full[st], tile >> 1))) break;
+            tc_fence_after();
+          }
+          const auto turn = [&](int x, int32_t mine) {
+            if (u > 0 && u <= mine) {
+              const uint32_t sv = st ^ 1;
+              if (x == 0 || s0 < u)                    // the first to read these values
+                if (!(ok = wait(&sh.v_full[sv], (tile - 1) >> 1))) return;
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                if (!(ok = wait(&sh.p_full[x][half], ns[x]))) return;
+                tc_fence_after();
+                pv(x, sv, half, u > 1);
+              }
+              ++ns[x];
             }
-            if (u + 1 < s0) qk(0, (ns[0] + 1) & 1, tile & 1, half);
-            if (u + 1 < s1) qk(1, (ns[1] + 1) & 1, tile & 1, half);
-            if (half || u + 2 == steps) commit(&sh.k_empty[tile & 1]);
-          }
-          if (!(u & 1) && !(ok = wait(&sh.v_full[tiles & 1], tiles >> 1))) break;
-          if (u < s0) {
-            if (!(ok = wait(&sh.p_full[0][ns[0] & 1], ns[0] >> 1))) break;
-            tc_fence_after();
-            pv(0, ns[0] & 1, tiles & 1, u & 1, u > 0);
-            ++ns[0];
-          }
-          if (u < s1) {
-            if (!(ok = wait(&sh.p_full[1][ns[1] & 1], ns[1] >> 1))) break;
-            tc_fence_after();
-            pv(1, ns[1] & 1, tiles & 1, u & 1, u > 0);
-            ++ns[1];
-          }
-          if ((u & 1) || u + 1 == steps) {
-            commit(&sh.v_empty[tiles & 1]);
-            ++tiles;
-          }
+            if (u < mine) {
+              if (u == 0) {
+                if (!(ok = wait(&sh.q_full[x], x ? nq1++ : items))) return;
+                tc_fence_after();
+              }
+              qk(x, st);
+            }
+          };
+          turn(0, s0);
+          if (!ok) break;
+          if (s1 > 0) turn(1, s1);
+          if (!ok) break;
+          if (u > 0) commit(&sh.v_empty[st ^ 1]);
+          if (u < steps) commit(&sh.k_empty[st]);
         }
+        tiles += steps;
       }
       commit(&sh.drained);                     // nothing of it runs on when memory is given back
       if (!mbar_wait_limit(&sh.drained, 0, abort, kWaitLimitNs)) {
@@ -529,8 +532,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     const int x = warp >> 2;                        // which tile of rows
     const int row = (warp & 3) * 32 + lane;         // of it, and lane of tensor memory
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t t_s = tmem + lanes + x * 2 * kStepTokens;
-    const uint32_t t_o = tmem + lanes + 4 * kStepTokens + x * D;
+    const uint32_t t_s = tmem + lanes + x * kTileTokens;
+    const uint32_t t_o = tmem + lanes + 2 * kTileTokens + x * D;
     uint32_t items = 0, tiles = 0, ns = 0;          // of the CTA; steps of this tile of rows
     bool ok = true;
 
@@ -628,110 +631,114 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
 
       float m = -INFINITY, sum = 0.0f;
       for (int32_t u = 0; u < n_steps; ++u, ++ns) {
-        const uint32_t buf = ns & 1;
-        if (u + 1 == n_steps) {                     // what follows, on its way
-          known = take(false);
-          if (known) fetch(0);
-        }
-        if (!(ok = wait(&sh.s_full[x][buf], ns >> 1))) break;
+        if (!(ok = wait(&sh.s_full[x], ns))) break;
         tc_fence_after();
-        const float4* scales =
-            sh.scales[(tile_base + (u >> 1)) & (kScaleRing - 1)] + (u & 1) * kStepGroups;
-        const int32_t t0 = it.tile0 * kTileTokens + u * kStepTokens;
-        uint32_t a[kStepTokens];
-        tmem_ld_32x32b_x32(t_s + buf * kStepTokens, *reinterpret_cast<uint32_t(*)[32]>(a));
-        tmem_ld_32x32b_x32(t_s + buf * kStepTokens + 32, *reinterpret_cast<uint32_t(*)[32]>(a + 32));
-        float by[kStepGroups], lv[kStepGroups];
-#pragma unroll
-        for (int g = 0; g < kStepGroups; ++g) {
-          by[g] = factor(scales[g].x, qs);
-          lv[g] = scales[g].y;
-        }
-        tmem_ld_wait();
-        if (t0 < from || t0 + kStepTokens - 1 > to) {
-          const int32_t last = top - t0, first = bottom - t0;
-#pragma unroll
-          for (int e = 0; e < kStepTokens; ++e)
-            if (e > last || e < first) a[e] = 0xff800000u;  // -inf
-        }
-        // ---- the maximum of acc * c + lv
-        float b[kStepGroups];
-#pragma unroll
-        for (int g = 0; g < kStepGroups; ++g) b[g] = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 16; e += 2)
-#pragma unroll
-          for (int g = 0; g < kStepGroups; ++g)
-            b[g] = fmaxf(b[g], fmaxf(__uint_as_float(a[g * 16 + e]),
-                                     __uint_as_float(a[g * 16 + e + 1])));
-        float most = -INFINITY;
-#pragma unroll
-        for (int g = 0; g < kStepGroups; ++g) most = fmaxf(most, fmaf(b[g], by[g], lv[g]));
-        if (__any_sync(0xffffffffu, most > m + kTilesLag)) {
-          const float now = fmaxf(m, most);
-          const float f = m == -INFINITY ? 0.0f : fast_exp2(m - now);
-          m = now;
-          sum *= f;
-          if (u > 0) {
-            if (!(ok = wait(&sh.o_full[x][(ns - 1) & 1], (ns - 1) >> 1))) break;
-            tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-              uint32_t o[16];
-              tmem_ld_32x32b_x16(t_o + c * 16, o);
-              tmem_ld_wait();
+        for (int half = 0; half < 2; ++half) {
+          const float4* scales =
+              sh.scales[(tile_base + u) & (kScaleRing - 1)] + half * kHalfGroups;
+          const int32_t t0 = (it.tile0 + u) * kTileTokens + half * kHalfTokens;
+          uint32_t a[kHalfTokens];
+          tmem_ld_32x32b_x32(t_s + half * kHalfTokens, *reinterpret_cast<uint32_t(*)[32]>(a));
+          tmem_ld_32x32b_x32(t_s + half * kHalfTokens + 32,
+                             *reinterpret_cast<uint32_t(*)[32]>(a + 32));
+          float by[kHalfGroups], lv[kHalfGroups];
 #pragma unroll
-              for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-              tmem_st_32x32b_x16(t_o + c * 16, o);
+          for (int g = 0; g < kHalfGroups; ++g) {
+            by[g] = factor(scales[g].x, qs);
+            lv[g] = scales[g].y;
+          }
+          tmem_ld_wait();
+          if (t0 < from || t0 + kHalfTokens - 1 > to) {
+            const int32_t last = top - t0, first = bottom - t0;
+#pragma unroll
+            for (int e = 0; e < kHalfTokens; ++e)
+              if (e > last || e < first) a[e] = 0xff800000u;  // -inf
+          }
+          // ---- the maximum of acc * c + lv
+          float b[kHalfGroups];
+#pragma unroll
+          for (int g = 0; g < kHalfGroups; ++g) b[g] = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 16; e += 2)
+#pragma unroll
+            for (int g = 0; g < kHalfGroups; ++g)
+              b[g] = fmaxf(b[g], fmaxf(__uint_as_float(a[g * 16 + e]),
+                                       __uint_as_float(a[g * 16 + e + 1])));
+          float most = -INFINITY;
+#pragma unroll
+          for (int g = 0; g < kHalfGroups; ++g) most = fmaxf(most, fmaf(b[g], by[g], lv[g]));
+          if (__any_sync(0xffffffffu, most > m + kTilesLag)) {
+            const float now = fmaxf(m, most);
+            const float f = m == -INFINITY ? 0.0f : fast_exp2(m - now);
+            m = now;
+            sum *= f;
+            if (u > 0 || half > 0) {                  // once the last half's product is done
+              if (!(ok = half ? wait(&sh.o_full[x][0], ns) : wait(&sh.o_full[x][1], ns - 1))) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < D / 16; ++c) {
+                uint32_t o[16];
+                tmem_ld_32x32b_x16(t_o + c * 16, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tmem_st_32x32b_x16(t_o + c * 16, o);
+              }
             }
           }
-        }
-        // ---- the weights
-        const float shift = m == -INFINITY ? 0.0f : kTilesShift - m;
-        uint64_t part[kStepGroups];
+          // ---- the weights
+          const float shift = m == -INFINITY ? 0.0f : kTilesShift - m;
+          uint64_t part[kHalfGroups];
 #pragma unroll
-        for (int g = 0; g < kStepGroups; ++g) part[g] = 0;
+          for (int g = 0; g < kHalfGroups; ++g) part[g] = 0;
 #pragma unroll
-        for (int c = 0; c < kStepGroups / 2; ++c) {
-          uint32_t w[16];
+          for (int c = 0; c < 2; ++c) {
+            uint32_t w[16];
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            const int g = c * 2 + y;
-            const float add = lv[g] + shift;
-            const uint64_t by2 = pack_f32x2(by[g], by[g]), add2 = pack_f32x2(add, add);
+            for (int y = 0; y < 2; ++y) {
+              const int g = c * 2 + y;
+              const float add = lv[g] + shift;
+              const uint64_t by2 = pack_f32x2(by[g], by[g]), add2 = pack_f32x2(add, add);
 #pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-              const int k = g * 16 + e;
-              float z0, z1;
-              unpack_f32x2(fma_f32x2(pack_b32x2(a[k], a[k + 1]), by2, add2), z0, z1);
-              z0 = fast_exp2(z0);
-              z1 = fast_exp2(z1);
-              part[g] = add_f32x2(part[g], pack_f32x2(z0, z1));
-              w[y * 8 + e / 2] = half2_of(z0, z1);
+              for (int e = 0; e < 16; e += 2) {
+                const int k = g * 16 + e;
+                float z0, z1;
+                unpack_f32x2(fma_f32x2(pack_b32x2(a[k], a[k + 1]), by2, add2), z0, z1);
+                z0 = fast_exp2(z0);
+                z1 = fast_exp2(z1);
+                part[g] = add_f32x2(part[g], pack_f32x2(z0, z1));
+                w[y * 8 + e / 2] = half2_of(z0, z1);
+              }
             }
+            tmem_st_32x32b_x16(t_s + half * 32 + c * 16, w);
           }
-          tmem_st_32x32b_x16(t_s + buf * kStepTokens + c * 16, w);
-        }
 #pragma unroll
-        for (int g = 0; g < kStepGroups; ++g) {
-          float p0, p1;
-          unpack_f32x2(part[g], p0, p1);
-          sum = fmaf(p0 + p1, scales[g].z, sum);
+          for (int g = 0; g < kHalfGroups; ++g) {
+            float p0, p1;
+            unpack_f32x2(part[g], p0, p1);
+            sum = fmaf(p0 + p1, scales[g].z, sum);
+          }
+          tmem_st_wait();
+          tc_fence_before();
+          mbar_arrive(&sh.p_full[x][half]);  // (after the second: the scales' place may be written)
         }
-        tmem_st_wait();
-        tc_fence_before();
-        mbar_arrive(&sh.p_full[x][buf]);            // (the scales' place may be written from here on)
+        if (!ok) break;
       }
       if (!ok) break;
 
       // ---- the output, after the next item's queries
-      if (known && next.more) put_all();
+      known = take(false);
+      if (known && next.more) {
+        fetch(0);
+        put_all();
+      }
       const bool none = sum == 0.0f;
       const float inv = none ? 0.0f : __fdividef(1.0f, sum);
       if (p.lse && rows0 + row < it.rows)
         p.lse[output_row(it, rows0 + row)] =
             none ? -INFINITY : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
-      if (!(ok = wait(&sh.o_full[x][(ns - 1) & 1], (ns - 1) >> 1))) break;
+      if (!(ok = wait(&sh.o_full[x][1], ns - 1))) break;
       tc_fence_after();
       // 32 of dim at a time through shared memory: a thread has a row, a store 64 bytes of eight
       const uint32_t stage = base + L::kOut + warp * 2048;
