@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
 #pragma unroll
             for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
             m = fmaxf(m, mx[nt][e]);
-            const float f = m == -INFINITY ? 1.0f : exp2f(mx[nt][e] - m);
+            const float f = m == -INFINITY ? 1.0f : fast_exp2(mx[nt][e] - m);
             mx[nt][e] = m;
             sum[nt][e] *= f;
 #pragma unroll
@@ -470,7 +470,7 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               float& z = s[mt][nt][2 * x + e];
-              z = exp2f(z - m);
+              z = fast_exp2(z - m);
               sum[nt][e] += z;
               z *= ratio;
             }
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
 #pragma unroll
         for (int w = 0; w < kAttWarps; ++w) m = fmaxf(m, m_s[w][nt * 8 + 2 * c + e]);
         big[nt][e] = m;
-        const float f = mx[nt][e] == -INFINITY ? 0.0f : exp2f(mx[nt][e] - m);
+        const float f = mx[nt][e] == -INFINITY ? 0.0f : fast_exp2(mx[nt][e] - m);
         sum[nt][e] *= f;
 #pragma unroll
         for (int hf = 0; hf < HALVES; ++hf)
@@ -569,7 +569,7 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
     }
     const bool all_of_it = seg_tile == at.tile0 && ends;
     // Output of rows by threads that hold values of dim 16 g + 2 k + {0, 1} (D = 64: 8 g + ...)
-    const auto write = [&](int k0, int k1) {
+    const auto write = [&]() {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -579,40 +579,59 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
           const int i = row / p.G, j = row - i * p.G;
           const int64_t r = (int64_t)(at.q0 + i) * (p.H * p.G) + at.h * p.G + j;
           const float l = sum[nt][e];
-          const float inv = l > 0.0f ? __fdividef(1.0f, l) : (l == 0.0f ? 0.0f : l);
+          const bool none = l == 0.0f;
+          const float inv = none ? 0.0f : __fdividef(1.0f, l);
 #pragma unroll
           for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
-              if (k >= k0 && k < k1)
-                attend_store2(p.out + r * D + hf * 128 + g * (2 * KS) + 2 * k, p.fp16,
-                              o[hf][k][nt][e] * inv, o[hf][k][nt][2 + e] * inv);
-          if (g == 0 && k0 == 0 && p.lse)
-            p.lse[r] = l == 0.0f ? -INFINITY
-                                 : (big[nt][e] - kShift + log2f(l)) * 0.69314718055994531f;
+            for (int k = 0; k < KS; k += 4) {
+              uint32_t w[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                w[q] = none ? 0u
+                            : attend_pack2(p.fp16, o[hf][k + q][nt][e] * inv,
+                                           o[hf][k + q][nt][2 + e] * inv);
+              *reinterpret_cast<uint4*>(p.out + r * D + hf * 128 + g * (2 * KS) + 2 * k) =
+                  make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          if (g == 0 && p.lse)
+            p.lse[r] = none ? -INFINITY : (big[nt][e] - kShift + log2f(l)) * 0.69314718055994531f;
         }
     };
     if (all_of_it) {
-      if (warp == 0) write(0, KS);
+      if (warp == 0) write();
     } else {
       // Partial results: the part that begins at this CTA's first unit in its slot 0, one that
-      // begins later (and so runs past its last) in slot 1.
+      // begins later (and so runs past its last) in slot 1.  A slot is its rows' maxima, their
+      // sums, and the sums of weighted values [row][dim].
       const int64_t first = u_begin + u - (at.tile - at.tile0);       // units of the whole
       const int64_t last = first + (at.tile_end - at.tile0) - 1;
       const int32_t c0 = (int32_t)(((first + 1) * E - 1) / U), c1 = (int32_t)(((last + 1) * E - 1) / U);
-      constexpr int PS = (NO + 4 * NT) * 32;
-      const auto slot_of = [&](int32_t cta) {
-        return p.partial + ((int64_t)cta * 2 + (cta == c0 && first > U * cta / E ? 1 : 0)) * PS + lane;
+      constexpr int PS = ROWS * (D + 2);
+      const int32_t odd = first > U * c0 / E ? 1 : 0;                 // the first part's slot
+      const auto slot_of = [&](int32_t k) {                           // of part k
+        return p.partial + ((int64_t)(c0 + k) * 2 + (k == 0 ? odd : 0)) * PS;
       };
       if (warp == 0) {
-        float* d = slot_of(blockIdx.x);
+        float* d = slot_of((int32_t)blockIdx.x - c0);
 #pragma unroll
-        for (int i = 0; i < NO; ++i) __stcg(d + i * 32, (&o[0][0][0][0])[i]);
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) {
-          __stcg(d + (NO + i) * 32, (&big[0][0])[i]);
-          __stcg(d + (NO + 2 * NT + i) * 32, (&sum[0][0])[i]);
-        }
+          for (int e = 0; e < 2; ++e) {
+            const int row = nt * 8 + 2 * c + e;
+            if (g == 0) {
+              __stcg(d + row, big[nt][e]);
+              __stcg(d + ROWS + row, sum[nt][e]);
+            }
+#pragma unroll
+            for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+              for (int k = 0; k < KS; k += 2)
+                __stcg(reinterpret_cast<float4*>(d + 2 * ROWS + row * D + hf * 128 +
+                                                 g * (2 * KS) + 2 * k),
+                       make_float4(o[hf][k][nt][e], o[hf][k][nt][2 + e], o[hf][k + 1][nt][e],
+                                   o[hf][k + 1][nt][2 + e]));
+          }
         __threadfence();
         __syncwarp();
         if (lane == 0) last_s = atomicAdd(p.counters + c0, 1u) == (unsigned)(c1 - c0);
@@ -621,56 +640,61 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
       if (last_s) {                                       // everyone else has left its part
         __threadfence();
         const int32_t parts = c1 - c0 + 1;
+        constexpr int TR = kAttThreads / ROWS;            // threads of a row
+        constexpr int DV = D / TR;                        // values of a thread
+        const int row = tid / TR, t = tid % TR;
+        float m = -INFINITY;
+        for (int32_t k = t; k < parts; k += TR) m = fmaxf(m, __ldcg(slot_of(k) + row));
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) {
-          (&big[0][0])[i] = -INFINITY;
-          (&sum[0][0])[i] = 0.0f;
-        }
-        for (int32_t k = 0; k < parts; ++k) {
-          const float* d = slot_of(c0 + k);
+        for (int x = 1; x < TR; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+        float acc[DV], l = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 2 * NT; ++i)
-            (&big[0][0])[i] = fmaxf((&big[0][0])[i], __ldcg(d + (NO + i) * 32));
-        }
-        // a warp merges its share of dim
-        constexpr int KW = KS / kAttWarps;                // tiles of dim of each piece
-        float acc[HALVES][KW][NT][4];
+        for (int i = 0; i < DV; ++i) acc[i] = 0.0f;
+        constexpr int UN = DV > 16 ? 2 : 4;               // parts on their way at once
+        for (int32_t k0 = 0; k0 < parts; k0 += UN) {
+          float4 v[UN][DV / 4];
+          float pm[UN], pl[UN];
 #pragma unroll
-        for (int i = 0; i < HALVES * KW * NT * 4; ++i) (&acc[0][0][0][0])[i] = 0.0f;
-        for (int32_t k = 0; k < parts; ++k) {
-          const float* d = slot_of(c0 + k);
-          float f[NT][2];
+          for (int y = 0; y < UN; ++y) {
+            const bool in = k0 + y < parts;
+            const float* d = slot_of(in ? k0 + y : k0);
+            pm[y] = in ? __ldcg(d + row) : -INFINITY;
+            pl[y] = __ldcg(d + ROWS + row);
 #pragma unroll
-          for (int i = 0; i < 2 * NT; ++i) {
-            const float m = __ldcg(d + (NO + i) * 32);
-            (&f[0][0])[i] = m == -INFINITY ? 0.0f : exp2f(m - (&big[0][0])[i]);
-            (&sum[0][0])[i] += (&f[0][0])[i] * __ldcg(d + (NO + 2 * NT + i) * 32);
+            for (int i = 0; i < DV / 4; ++i)
+              v[y][i] = __ldcg(reinterpret_cast<const float4*>(d + 2 * ROWS + row * D) + i * TR + t);
           }
 #pragma unroll
-          for (int hf = 0; hf < HALVES; ++hf)
+          for (int y = 0; y < UN; ++y) {
+            const float f = pm[y] == -INFINITY ? 0.0f : fast_exp2(pm[y] - m);
+            l = fmaf(f, pl[y], l);
 #pragma unroll
-            for (int kk = 0; kk < KW; ++kk)
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  acc[hf][kk][nt][e] +=
-                      f[nt][e & 1] *
-                      __ldcg(d + (((hf * KS + warp * KW + kk) * NT + nt) * 4 + e) * 32);
-        }
-#pragma unroll
-        for (int w = 0; w < kAttWarps; ++w)
-          if (w == warp) {
-#pragma unroll
-            for (int hf = 0; hf < HALVES; ++hf)
-#pragma unroll
-              for (int kk = 0; kk < KW; ++kk)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) o[hf][w * KW + kk][nt][e] = acc[hf][kk][nt][e];
-            write(w * KW, (w + 1) * KW);
+            for (int i = 0; i < DV / 4; ++i) {
+              acc[4 * i] = fmaf(f, v[y][i].x, acc[4 * i]);
+              acc[4 * i + 1] = fmaf(f, v[y][i].y, acc[4 * i + 1]);
+              acc[4 * i + 2] = fmaf(f, v[y][i].z, acc[4 * i + 2]);
+              acc[4 * i + 3] = fmaf(f, v[y][i].w, acc[4 * i + 3]);
+            }
           }
+        }
+        const int full = at.group * ROWS + row;
+        if (full < at.n * p.G) {
+          const int i = full / p.G, j = full - i * p.G;
+          const int64_t r = (int64_t)(at.q0 + i) * (p.H * p.G) + at.h * p.G + j;
+          const bool none = l == 0.0f;
+          const float inv = none ? 0.0f : __fdividef(1.0f, l);
+#pragma unroll
+          for (int q = 0; q < DV / 4; ++q) {
+            uint2 w = make_uint2(0u, 0u);
+            if (!none) {
+              w.x = attend_pack2(p.fp16, acc[4 * q] * inv, acc[4 * q + 1] * inv);
+              w.y = attend_pack2(p.fp16, acc[4 * q + 2] * inv, acc[4 * q + 3] * inv);
+            }
+            *reinterpret_cast<uint2*>(p.out + r * D + (q * TR + t) * 4) = w;
+          }
+          if (t == 0 && p.lse)
+            p.lse[r] = none ? -INFINITY : (m - kShift + log2f(l)) * 0.69314718055994531f;
+        }
         if (tid == 0) p.counters[c0] = 0;                 // as the next call finds it
       }
       __syncthreads();
@@ -738,11 +762,10 @@ hs_status launch_dim(const AttendParams& p, int32_t dim, int64_t rows, cudaStrea
 
 }  // namespace
 
-// A slot holds (rows x dim) sums, and a maximum and a sum for each lane's rows.
 size_t attend_workspace(int32_t dim) {
-  constexpr int nt = 2;
+  constexpr int rows = 16;                                // of a tile, at most
   const int64_t ctas = (int64_t)num_sms() * kAttendMaxPerSm;
-  const int64_t slot = ((int64_t)dim / 16 * nt * 4 + 4 * nt) * 32 * 4;
+  const int64_t slot = (int64_t)rows * (dim + 2) * 4;
   return (size_t)(attend_counter_bytes() + ctas * 2 * slot);
 }
 

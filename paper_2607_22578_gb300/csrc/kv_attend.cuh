@@ -98,6 +98,13 @@ __device__ __forceinline__ void attend_load8(const uint16_t* src, int vec, int f
   attend_unpack8(vec ? __ldg(reinterpret_cast<const uint4*>(src)) : attend_raw8(src), fp16, f);
 }
 
+// 2^x to 2 units in the last place; below the normal range 0
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Two neighbouring outputs, rounded to nearest even
 __device__ __forceinline__ uint32_t attend_pack2(int fp16, float x0, float x1) {
   if (fp16) {
@@ -106,10 +113,6 @@ __device__ __forceinline__ uint32_t attend_pack2(int fp16, float x0, float x1) {
   }
   const __nv_bfloat162 h = __floats2bfloat162_rn(x0, x1);
   return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-__device__ __forceinline__ void attend_store2(uint16_t* dst, int fp16, float x0, float x1) {
-  *reinterpret_cast<uint32_t*>(dst) = attend_pack2(fp16, x0, x1);
 }
 
 }  // namespace hs

@@ -143,12 +143,6 @@ __device__ __forceinline__ bool elect_one() {
   return p != 0;
 }
 
-__device__ __forceinline__ float fast_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 // Two floats at once (sm_100's packed fp32 operations)
 __device__ __forceinline__ uint64_t pack_b32x2(uint32_t lo, uint32_t hi) {
   uint64_t r;
