@@ -8,8 +8,9 @@
 //
 // Reading the codes once is all the work there is (2 * dim bytes a token against 2 * G flops a
 // byte), so the kernel is built around keeping loads in flight:
-//  - The work is cut into units of 128 tokens of one (request, kv head, group of rows), laid end
-//    to end, and every CTA takes an equal share of the list, whatever the lengths are.  Where a
+//  - The work is cut into units of a few hundred tokens of one (request, kv head, group of rows),
+//    laid end to end, and every CTA (one an SM) takes an equal share of the list, whatever the
+//    lengths are.  Where a
 //    (request, head, group) is cut between CTAs, each leaves its partial result in the workspace
 //    and the one that comes last merges them in their order: no second launch, and a result that
 //    does not depend on which was last.
@@ -32,14 +33,22 @@ hs_status launch_kv_attend_tiles(const AttendParams&, int32_t, int32_t, cudaStre
 
 namespace {
 
-constexpr int kAttWarps = 4;
-constexpr int kAttThreads = kAttWarps * 32;
 constexpr int kWarpTokens = 32;                          // of a unit, for each warp
-constexpr int kUnitTokens = kAttWarps * kWarpTokens;
 constexpr int kAttStages = 2;
 constexpr int kFewRows = 32;                             // of a request: more are kv_attend_tiles.cu's
 constexpr float kLag = 8.0f;                             // of the running maximum, in powers of two
 constexpr float kShift = 7.0f;
+
+// Warps of a CTA, and CTAs of an SM.  Small CTAs side by side go on loading while one of them ends
+// a (request, head, group); a single large one leaves few parts of a long request to merge.
+template <int D, int NT>
+constexpr int few_warps() { return D == 256 ? 7 - NT : 4; }
+template <int D, int NT>
+constexpr int many_warps() { return D == 256 ? 7 - NT : NT == 1 || (D == 64 && NT == 2) ? 12 : 8; }
+template <int D, int NT, int WARPS>
+constexpr int attend_ctas() {
+  return WARPS > 4 ? 1 : D == 64 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : 4 - NT;
+}
 
 template <int D>
 constexpr int stage_bytes() { return 2 * kWarpTokens * D + 16; }  // K, V, two scales of each
@@ -94,118 +103,139 @@ __device__ __forceinline__ uint2 lds64(uint32_t a) {
 // A place in the list of units: a (request, kv head, group of rows) and one of its tiles.
 struct Place {
   int32_t r, h, group, groups;
-  int32_t tile, tile0, tile_end;   // tiles of kUnitTokens tokens
+  int32_t tile, tile0, tile_end;   // tiles of a CTA's tokens
   int32_t n, q0, len;
 };
 
 struct Request {
-  int32_t n, q0, len, groups, tile0, tiles;
+  int32_t n, q0, len, groups, tile0, tiles;  // tiles of a CTA's tokens
 };
 
 // What request r asks for; groups = 0 if nothing (or nothing that can be done: *bad).
-__device__ __forceinline__ Request request(const AttendParams& p, int32_t r, int32_t rows,
-                                           unsigned* bad) {
+template <int ROWS, int TOKENS>
+__device__ __forceinline__ Request request(const AttendParams& p, int32_t r, unsigned* bad) {
   Request q;
   q.groups = 0;
   q.tile0 = 0;
   q.tiles = 0;
   if (!attend_request(p, r, q.n, q.q0, q.len, bad)) return q;
   if (q.n * p.G > p.rows_most) return q;                // another kernel's
-  q.groups = (q.n * p.G + rows - 1) / rows;
+  q.groups = (q.n * p.G + ROWS - 1) / ROWS;
   if (p.window > 0) {
     const int32_t first = q.len - q.n - p.window + 1;
-    if (first > 0) q.tile0 = first / kUnitTokens;
+    if (first > 0) q.tile0 = first / TOKENS;
   }
-  q.tiles = max((q.len + kUnitTokens - 1) / kUnitTokens - q.tile0, 1);  // an empty one too
+  q.tiles = max((q.len + TOKENS - 1) / TOKENS - q.tile0, 1);  // an empty one too
   return q;
 }
 
-template <int D, int NT, int FMT>
-__global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendParams p) {
+template <int D, int NT, int WARPS, int FMT>
+__global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
+    kv_attend_kernel(const AttendParams p) {
+  constexpr int THREADS = WARPS * 32;
+  constexpr int TOKENS = WARPS * kWarpTokens;    // of a unit
   constexpr int ROWS = 8 * NT;
   constexpr int HALVES = D == 64 ? 1 : D / 128;  // 128-byte pieces of a row (D = 64: one of 64)
   constexpr int KS = D == 64 ? 4 : 8;            // k16 steps, and m16 tiles of dim, of a piece
   constexpr int NO = HALVES * KS * NT * 4;       // output registers of a thread
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int64_t sums[kAttWarps];
-  __shared__ int64_t found_units;
-  __shared__ int32_t found_r, last_s;
-  __shared__ float m_s[kAttWarps][ROWS];
+  __shared__ int32_t last_s;
+  __shared__ float m_s[WARPS][ROWS];
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, c = lane & 3;
   uint8_t* ring = smem + warp * (kAttStages * stage_bytes<D>());
-  float* merge = reinterpret_cast<float*>(smem + kAttWarps * kAttStages * stage_bytes<D>());
+  float* merge = reinterpret_cast<float*>(smem + WARPS * kAttStages * stage_bytes<D>());
   const uint32_t ring_u = smem_u32(ring);
 
   pdl_wait();
   pdl_trigger();
   const int32_t R = p.n_req_dev ? max(0, min(__ldg(p.n_req_dev), p.n_req)) : p.n_req;
 
-  // ---- how many units there are, and which are this CTA's
+  // ---- how many units there are, and which are this CTA's: each warp for itself, so that no
+  // barrier stands before the first loads
   unsigned bad = 0;
-  const int32_t per = (R + kAttThreads - 1) / kAttThreads;
-  const int32_t ra = min(tid * per, R), rb = min(ra + per, R);
-  int64_t mine = 0;
-  for (int32_t r = ra; r < rb; ++r) {
-    const Request q = request(p, r, ROWS, &bad);
-    mine += (int64_t)q.groups * q.tiles;
-  }
-  mine *= p.H;
-  int64_t incl = mine;
+  const auto units_of = [&](const Request& q) { return (int64_t)q.groups * q.tiles * p.H; };
+  // Of lanes' consecutive counts x: the total, and for the lane that holds number `at` of them the
+  // count before its own.
+  const auto scan = [&](int64_t x, int64_t& incl) {
+    incl = x;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += u;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t u = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += u;
+    }
+    return __shfl_sync(0xffffffffu, incl, 31);
+  };
+  const int32_t per = (R + 31) / 32;
+  Request mine{};
+  int64_t sum_mine = 0, incl;
+  for (int32_t r = lane * per; r < min((lane + 1) * per, R); ++r) {
+    mine = request<ROWS, TOKENS>(p, r, &bad);
+    sum_mine += units_of(mine);
   }
-  if (lane == 31) sums[warp] = incl;
-  __syncthreads();
-  int64_t U = 0, before = 0;
-#pragma unroll
-  for (int w = 0; w < kAttWarps; ++w) {
-    if (w == warp) before = U;
-    U += sums[w];
-  }
+  const int64_t U = scan(sum_mine, incl);
   const int64_t E = min((int64_t)gridDim.x, U);           // CTAs with work
   if (bad && blockIdx.x == 0) set_error(p.err, bad);
   if (blockIdx.x >= E) return;
   const int64_t u_begin = U * blockIdx.x / E, u_end = U * (blockIdx.x + 1) / E;
-  before += incl - mine;
-  if (u_begin >= before && u_begin < before + mine) {     // one thread's requests hold the first
-    int64_t at = before;
-    int32_t r = ra;
-    for (; r + 1 < rb; ++r) {
-      const Request q = request(p, r, ROWS, &bad);
-      const int64_t n = (int64_t)q.groups * q.tiles * p.H;
-      if (u_begin < at + n) break;
-      at += n;
+  int holder = __ffs(__ballot_sync(0xffffffffu, u_begin < incl)) - 1;  // its requests hold the first
+  int32_t start_r = holder * per;
+  int64_t skip = u_begin - __shfl_sync(0xffffffffu, incl - sum_mine, holder);
+  for (int32_t base = start_r; per > 1; base += 32) {     // ... and which of them does
+    const int32_t r = base + lane;
+    mine = Request{};
+    if (r < min(start_r + per, R)) mine = request<ROWS, TOKENS>(p, r, &bad);
+    const int64_t n = units_of(mine), all = scan(n, incl);
+    if (skip < all || base + 32 >= min(start_r + per, R)) {
+      const unsigned holds = __ballot_sync(0xffffffffu, skip < incl);
+      holder = holds ? __ffs(holds) - 1 : 31;
+      skip -= __shfl_sync(0xffffffffu, incl - n, holder);
+      start_r = base + holder;
+      break;
     }
-    found_r = r;
-    found_units = u_begin - at;
+    skip -= all;
   }
-  __syncthreads();
 
   Place fetch;                                            // what is loaded next
-  const auto open = [&](Place& w, int32_t r, int64_t skip) {
-    Request q{0, 0, 0, 1, 0, 1};                          // (of none, should the lengths change)
-    for (; r < R; ++r) {
-      const Request x = request(p, r, ROWS, &bad);
-      if (x.groups > 0) {
-        q = x;
-        break;
-      }
-    }
+  const auto enter = [&](Place& w, int32_t r, const Request& q) {
     w.r = r;
     w.groups = q.groups;
     w.n = q.n;
     w.q0 = q.q0;
     w.len = q.len;
-    w.tile0 = q.tile0;
+    w.tile0 = w.tile = q.tile0;
     w.tile_end = q.tile0 + q.tiles;
-    w.h = (int32_t)(skip / ((int64_t)q.groups * q.tiles));
-    skip -= (int64_t)w.h * q.groups * q.tiles;
-    w.group = (int32_t)(skip / q.tiles);
-    w.tile = q.tile0 + (int32_t)(skip - (int64_t)w.group * q.tiles);
+    w.h = w.group = 0;
+  };
+  {
+    Request q;
+    q.n = __shfl_sync(0xffffffffu, mine.n, holder);
+    q.q0 = __shfl_sync(0xffffffffu, mine.q0, holder);
+    q.len = __shfl_sync(0xffffffffu, mine.len, holder);
+    q.groups = __shfl_sync(0xffffffffu, mine.groups, holder);
+    q.tile0 = __shfl_sync(0xffffffffu, mine.tile0, holder);
+    q.tiles = __shfl_sync(0xffffffffu, mine.tiles, holder);
+    enter(fetch, start_r, q);
+    if (skip < q.tiles) {                                 // (of the first head and group, mostly)
+      fetch.tile += (int32_t)skip;
+    } else {
+      const int64_t part = skip / q.tiles;                // which (head, group)
+      fetch.tile += (int32_t)(skip - part * q.tiles);
+      fetch.h = (int32_t)(part / q.groups);
+      fetch.group = (int32_t)(part - (int64_t)fetch.h * q.groups);
+    }
+  }
+  const auto open = [&](Place& w, int32_t r) {            // the next request with work
+    Request q{0, 0, 0, 1, 0, 1};                          // (of none, should the lengths change)
+    for (; r < R; ++r) {
+      const Request x = request<ROWS, TOKENS>(p, r, &bad);
+      if (x.groups > 0) {
+        q = x;
+        break;
+      }
+    }
+    enter(w, r, q);
   };
   const auto step = [&](Place& w) {                       // to the next unit of the list
     if (++w.tile < w.tile_end) return;
@@ -213,21 +243,20 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
     if (++w.group < w.groups) return;
     w.group = 0;
     if (++w.h < p.H) return;
-    open(w, w.r + 1, 0);
+    open(w, w.r + 1);
   };
-  open(fetch, found_r, found_units);
 
   // ---- loading: this warp's 32 tokens of a unit, one stage
   const int two = p.bt_log2 == 4;                         // its tokens lie in two blocks
   int32_t id0 = 0, id1 = 0;
   const auto look_up = [&]() {                            // the blocks of `fetch`
-    const int32_t t0 = fetch.tile * kUnitTokens + warp * kWarpTokens;
+    const int32_t t0 = fetch.tile * TOKENS + warp * kWarpTokens;
     const int32_t* row = p.table + (int64_t)fetch.r * p.width + (t0 >> p.bt_log2);
     id0 = t0 < fetch.len ? __ldg(row) : 0;
     id1 = two && t0 + 16 < fetch.len ? __ldg(row + 1) : id0;
   };
   const auto load = [&](int stage) {
-    const int32_t t0 = fetch.tile * kUnitTokens + warp * kWarpTokens;
+    const int32_t t0 = fetch.tile * TOKENS + warp * kWarpTokens;
     int32_t left = fetch.len - t0;                        // tokens that there are
     if ((uint32_t)id0 >= (uint32_t)p.n_blocks || (uint32_t)id1 >= (uint32_t)p.n_blocks) {
       if (left > 0) set_error(p.err, kErrInvalidArg);
@@ -366,7 +395,7 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
                  : "=f"(scales[0]), "=f"(scales[1]), "=f"(scales[2]), "=f"(scales[3])
                  : "r"(kb + 2 * kWarpTokens * D)
                  : "memory");
-    const int32_t t0 = at.tile * kUnitTokens + warp * kWarpTokens;
+    const int32_t t0 = at.tile * TOKENS + warp * kWarpTokens;
     if (t0 < at.len) {
       // ---- s = q . k: tokens are M, rows are N
       float s[2][NT][4];
@@ -537,7 +566,7 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
       for (int e = 0; e < 2; ++e) {
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < kAttWarps; ++w) m = fmaxf(m, m_s[w][nt * 8 + 2 * c + e]);
+        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, m_s[w][nt * 8 + 2 * c + e]);
         big[nt][e] = m;
         const float f = mx[nt][e] == -INFINITY ? 0.0f : fast_exp2(mx[nt][e] - m);
         sum[nt][e] *= f;
@@ -550,20 +579,22 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
           }
       }
 #pragma unroll
-    for (int half = kAttWarps / 2; half > 0; half >>= 1) {
-      float* mine_s = merge + (warp % half) * (NO + 2 * NT) * 32 + lane;
-      if (warp >= half && warp < 2 * half) {
+    for (int live = WARPS; live > 1; live = (live + 1) / 2) {  // the upper half onto the lower
+      const int half = (live + 1) / 2;
+      if (warp >= half && warp < live) {
+        float* d = merge + (warp - half) * (NO + 2 * NT) * 32 + lane;
 #pragma unroll
-        for (int i = 0; i < NO; ++i) mine_s[i * 32] = (&o[0][0][0][0])[i];
+        for (int i = 0; i < NO; ++i) d[i * 32] = (&o[0][0][0][0])[i];
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) mine_s[(NO + i) * 32] = (&sum[0][0])[i];
+        for (int i = 0; i < 2 * NT; ++i) d[(NO + i) * 32] = (&sum[0][0])[i];
       }
       __syncthreads();
-      if (warp < half) {
+      if (warp < live - half) {
+        const float* d = merge + warp * (NO + 2 * NT) * 32 + lane;
 #pragma unroll
-        for (int i = 0; i < NO; ++i) (&o[0][0][0][0])[i] += mine_s[i * 32];
+        for (int i = 0; i < NO; ++i) (&o[0][0][0][0])[i] += d[i * 32];
 #pragma unroll
-        for (int i = 0; i < 2 * NT; ++i) (&sum[0][0])[i] += mine_s[(NO + i) * 32];
+        for (int i = 0; i < 2 * NT; ++i) (&sum[0][0])[i] += d[(NO + i) * 32];
       }
       __syncthreads();
     }
@@ -640,61 +671,58 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
       if (last_s) {                                       // everyone else has left its part
         __threadfence();
         const int32_t parts = c1 - c0 + 1;
-        constexpr int TR = kAttThreads / ROWS;            // threads of a row
-        constexpr int DV = D / TR;                        // values of a thread
-        const int row = tid / TR, t = tid % TR;
-        float m = -INFINITY;
-        for (int32_t k = t; k < parts; k += TR) m = fmaxf(m, __ldcg(slot_of(k) + row));
+        constexpr int UN = 10;                            // parts on their way at once
+        for (int f = tid; f < ROWS * D / 4; f += THREADS) {  // four values of a row
+          const int row = f / (D / 4);
+          const int full = at.group * ROWS + row;
+          if (full >= at.n * p.G) continue;
+          float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          float m = -INFINITY, l = 0.0f;
+          for (int32_t k0 = 0; k0 < parts; k0 += UN) {
+            float4 v[UN];
+            float pm[UN], pl[UN];
 #pragma unroll
-        for (int x = 1; x < TR; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-        float acc[DV], l = 0.0f;
+            for (int y = 0; y < UN; ++y) {
+              const bool in = k0 + y < parts;
+              const float* d = slot_of(in ? k0 + y : k0);
+              pm[y] = in ? __ldcg(d + row) : -INFINITY;
+              pl[y] = __ldcg(d + ROWS + row);
+              v[y] = __ldcg(reinterpret_cast<const float4*>(d + 2 * ROWS) + f);
+            }
+            float now = m;
 #pragma unroll
-        for (int i = 0; i < DV; ++i) acc[i] = 0.0f;
-        constexpr int UN = DV > 16 ? 2 : 4;               // parts on their way at once
-        for (int32_t k0 = 0; k0 < parts; k0 += UN) {
-          float4 v[UN][DV / 4];
-          float pm[UN], pl[UN];
+            for (int y = 0; y < UN; ++y) now = fmaxf(now, pm[y]);
+            const float back = m == -INFINITY ? 0.0f : fast_exp2(m - now);
+            m = now;
+            l *= back;
+            acc.x *= back;
+            acc.y *= back;
+            acc.z *= back;
+            acc.w *= back;
 #pragma unroll
-          for (int y = 0; y < UN; ++y) {
-            const bool in = k0 + y < parts;
-            const float* d = slot_of(in ? k0 + y : k0);
-            pm[y] = in ? __ldcg(d + row) : -INFINITY;
-            pl[y] = __ldcg(d + ROWS + row);
-#pragma unroll
-            for (int i = 0; i < DV / 4; ++i)
-              v[y][i] = __ldcg(reinterpret_cast<const float4*>(d + 2 * ROWS + row * D) + i * TR + t);
-          }
-#pragma unroll
-          for (int y = 0; y < UN; ++y) {
-            const float f = pm[y] == -INFINITY ? 0.0f : fast_exp2(pm[y] - m);
-            l = fmaf(f, pl[y], l);
-#pragma unroll
-            for (int i = 0; i < DV / 4; ++i) {
-              acc[4 * i] = fmaf(f, v[y][i].x, acc[4 * i]);
-              acc[4 * i + 1] = fmaf(f, v[y][i].y, acc[4 * i + 1]);
-              acc[4 * i + 2] = fmaf(f, v[y][i].z, acc[4 * i + 2]);
-              acc[4 * i + 3] = fmaf(f, v[y][i].w, acc[4 * i + 3]);
+            for (int y = 0; y < UN; ++y) {
+              const float w = pm[y] == -INFINITY ? 0.0f : fast_exp2(pm[y] - m);
+              l = fmaf(w, pl[y], l);
+              acc.x = fmaf(w, v[y].x, acc.x);
+              acc.y = fmaf(w, v[y].y, acc.y);
+              acc.z = fmaf(w, v[y].z, acc.z);
+              acc.w = fmaf(w, v[y].w, acc.w);
             }
           }
-        }
-        const int full = at.group * ROWS + row;
-        if (full < at.n * p.G) {
           const int i = full / p.G, j = full - i * p.G;
           const int64_t r = (int64_t)(at.q0 + i) * (p.H * p.G) + at.h * p.G + j;
           const bool none = l == 0.0f;
           const float inv = none ? 0.0f : __fdividef(1.0f, l);
-#pragma unroll
-          for (int q = 0; q < DV / 4; ++q) {
-            uint2 w = make_uint2(0u, 0u);
-            if (!none) {
-              w.x = attend_pack2(p.fp16, acc[4 * q] * inv, acc[4 * q + 1] * inv);
-              w.y = attend_pack2(p.fp16, acc[4 * q + 2] * inv, acc[4 * q + 3] * inv);
-            }
-            *reinterpret_cast<uint2*>(p.out + r * D + (q * TR + t) * 4) = w;
+          uint2 w = make_uint2(0u, 0u);
+          if (!none) {
+            w.x = attend_pack2(p.fp16, acc.x * inv, acc.y * inv);
+            w.y = attend_pack2(p.fp16, acc.z * inv, acc.w * inv);
           }
-          if (t == 0 && p.lse)
+          *reinterpret_cast<uint2*>(p.out + r * D + (f - row * (D / 4)) * 4) = w;
+          if (f == row * (D / 4) && p.lse)
             p.lse[r] = none ? -INFINITY : (m - kShift + log2f(l)) * 0.69314718055994531f;
         }
+        __syncthreads();
         if (tid == 0) p.counters[c0] = 0;                 // as the next call finds it
       }
       __syncthreads();
@@ -705,52 +733,45 @@ __global__ void __launch_bounds__(kAttThreads) kv_attend_kernel(const AttendPara
   if (bad) set_error(p.err, bad);
 }
 
-template <int D, int NT>
+template <int D, int NT, int WARPS>
 constexpr size_t attend_smem() {
   constexpr int NO = D / 16 * NT * 4;
-  return (size_t)kAttWarps * kAttStages * stage_bytes<D>() +
-         (size_t)(kAttWarps / 2) * (NO + 2 * NT) * 32 * 4;
+  return (size_t)WARPS * kAttStages * stage_bytes<D>() +
+         (size_t)(WARPS / 2) * (NO + 2 * NT) * 32 * 4;
 }
 
-// CTAs of a launch: as many as run at once.
-template <int D, int NT, int FMT>
-hs_status residents(int& ctas) {
-  static std::atomic<int> per_sm[kMaxDeviceOrdinals];
-  const int dev = device_ordinal();
-  int n = dev >= 0 ? per_sm[dev].load(std::memory_order_acquire) : 0;
-  if (n == 0) {
-    const auto kernel = kv_attend_kernel<D, NT, FMT>;
-    constexpr int smem = (int)attend_smem<D, NT>();
-    if (const hs_status st = cuda_fail(
-            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem),
-            "kv_attend shared memory"))
-      return st;
-    if (const hs_status st = cuda_fail(
-            cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, kAttThreads, smem),
-            "kv_attend occupancy"))
-      return st;
-    if (n < 1) return fail(HS_ERR_CUDA, "kv_attend does not fit an SM");
-    if (n > kAttendMaxPerSm) n = kAttendMaxPerSm;
-    if (dev >= 0) per_sm[dev].store(n, std::memory_order_release);
-  }
-  ctas = n * num_sms();
-  return HS_OK;
-}
-
-template <int D, int NT, int FMT>
+template <int D, int NT, int WARPS, int FMT>
 hs_status launch(const AttendParams& p, cudaStream_t stream) {
-  int ctas = 0;
-  if (const hs_status st = residents<D, NT, FMT>(ctas)) return st;
-  launch_pdl(kv_attend_kernel<D, NT, FMT>, dim3((unsigned)ctas), dim3(kAttThreads),
-             attend_smem<D, NT>(), stream, p);
+  constexpr int smem = (int)attend_smem<D, NT, WARPS>();
+  static std::atomic<uint64_t> configured{0};
+  const hs_status st = once_per_device(configured, [] {
+    return cuda_fail(cudaFuncSetAttribute(kv_attend_kernel<D, NT, WARPS, FMT>,
+                                          cudaFuncAttributeMaxDynamicSharedMemorySize, smem),
+                     "kv_attend shared memory");
+  });
+  if (st != HS_OK) return st;
+  launch_pdl(kv_attend_kernel<D, NT, WARPS, FMT>,
+             dim3((unsigned)(num_sms() * attend_ctas<D, NT, WARPS>())), dim3(WARPS * 32), smem,
+             stream, p);
   count_launches(1);
   return cuda_fail(cudaGetLastError(), "kv_attend launch");
 }
 
+template <int D, int NT, int FMT>
+hs_status launch_warps(const AttendParams& p, int64_t rows, cudaStream_t stream) {
+  // (request, head, group)s, at most
+  const int64_t whole = (int64_t)p.n_req * p.H * ((rows + 8 * NT - 1) / (8 * NT));
+  return whole * 4 <= num_sms() ? launch<D, NT, many_warps<D, NT>(), FMT>(p, stream)
+                                : launch<D, NT, few_warps<D, NT>(), FMT>(p, stream);
+}
+
 template <int D, int FMT>
 hs_status launch_rows(const AttendParams& p, int64_t rows, cudaStream_t stream) {
-  if (rows <= 8) return launch<D, 1, FMT>(p, stream);
-  return launch<D, 2, FMT>(p, stream);
+  if (rows <= 8) return launch_warps<D, 1, FMT>(p, rows, stream);
+  // With dim = 64 there are registers for 32 rows: the codes are read and decoded once for them.
+  if constexpr (D == 64)
+    if (rows > 16) return launch_warps<D, 4, FMT>(p, rows, stream);
+  return launch_warps<D, 2, FMT>(p, rows, stream);
 }
 
 template <int FMT>
@@ -763,9 +784,9 @@ hs_status launch_dim(const AttendParams& p, int32_t dim, int64_t rows, cudaStrea
 }  // namespace
 
 size_t attend_workspace(int32_t dim) {
-  constexpr int rows = 16;                                // of a tile, at most
+  const int64_t rows = dim == 64 ? 32 : 16;               // of a tile, at most
   const int64_t ctas = (int64_t)num_sms() * kAttendMaxPerSm;
-  const int64_t slot = (int64_t)rows * (dim + 2) * 4;
+  const int64_t slot = rows * (dim + 2) * 4;
   return (size_t)(attend_counter_bytes() + ctas * 2 * slot);
 }
 

@@ -42,6 +42,7 @@ struct AttendParams {
 
 constexpr int kAttendMaxPerSm = 4;  // CTAs of a launch that one SM holds, at most
 
+// A counter for each CTA of a launch.
 inline int64_t attend_counter_bytes() {
   return ((int64_t)num_sms() * kAttendMaxPerSm * 4 + 255) / 256 * 256;
 }
