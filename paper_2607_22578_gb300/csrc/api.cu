@@ -645,6 +645,11 @@ hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, i
   p.n_blocks = (int32_t)cache->n_blocks;
   p.H = cache->n_kv_heads;
   p.G = n_heads / cache->n_kv_heads;
+  // (rows go up to a tile's 256 past the last)
+  const int64_t most_rows = (int64_t)max_q * p.G + 256;
+  p.G_inv = p.G > 1 && most_rows * p.G < 0x100000000LL
+                ? (uint32_t)((0x100000000LL + p.G - 1) / p.G)
+                : 0u;
   p.bt_log2 = block_log2(cache->block_tokens);
   p.q = static_cast<const uint16_t*>(q);
   p.q_token = token_stride;

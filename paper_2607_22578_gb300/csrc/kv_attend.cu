@@ -167,34 +167,73 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
     }
     return __shfl_sync(0xffffffffu, incl, 31);
   };
-  const int32_t per = (R + 31) / 32;
-  Request mine{};
-  int64_t sum_mine = 0, incl;
-  for (int32_t r = lane * per; r < min((lane + 1) * per, R); ++r) {
-    mine = request<ROWS, TOKENS>(p, r, &bad);
-    sum_mine += units_of(mine);
-  }
-  const int64_t U = scan(sum_mine, incl);
-  const int64_t E = min((int64_t)gridDim.x, U);           // CTAs with work
-  if (bad && blockIdx.x == 0) set_error(p.err, bad);
-  if (blockIdx.x >= E) return;
-  const int64_t u_begin = U * blockIdx.x / E, u_end = U * (blockIdx.x + 1) / E;
-  int holder = __ffs(__ballot_sync(0xffffffffu, u_begin < incl)) - 1;  // its requests hold the first
-  int32_t start_r = holder * per;
-  int64_t skip = u_begin - __shfl_sync(0xffffffffu, incl - sum_mine, holder);
-  for (int32_t base = start_r; per > 1; base += 32) {     // ... and which of them does
-    const int32_t r = base + lane;
-    mine = Request{};
-    if (r < min(start_r + per, R)) mine = request<ROWS, TOKENS>(p, r, &bad);
-    const int64_t n = units_of(mine), all = scan(n, incl);
-    if (skip < all || base + 32 >= min(start_r + per, R)) {
-      const unsigned holds = __ballot_sync(0xffffffffu, skip < incl);
-      holder = holds ? __ffs(holds) - 1 : 31;
-      skip -= __shfl_sync(0xffffffffu, incl - n, holder);
-      start_r = base + holder;
-      break;
+  int64_t U, u_begin, u_end, E, skip;
+  int32_t start_r;
+  const auto share = [&]() {                              // of U units
+    E = min((int64_t)gridDim.x, U);                       // CTAs with work
+    u_begin = U * blockIdx.x / E;
+    u_end = U * (blockIdx.x + 1) / E;
+  };
+  constexpr int CHUNKS = 4;
+  if (R <= 32 * CHUNKS) {                                 // a lane's requests are 32 apart
+    int64_t n[CHUNKS], incl[CHUNKS], all[CHUNKS];
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) {
+      Request q{};
+      if (k * 32 + lane < R) q = request<ROWS, TOKENS>(p, k * 32 + lane, &bad);
+      n[k] = units_of(q);
     }
-    skip -= all;
+    U = 0;
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) {
+      all[k] = 0;
+      incl[k] = 0;
+      if (k * 32 < R) all[k] = scan(n[k], incl[k]);
+      U += all[k];
+    }
+    if (bad && blockIdx.x == 0) set_error(p.err, bad);
+    if (blockIdx.x >= U) return;
+    share();
+    skip = u_begin;
+    start_r = 0;
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) {
+      if (!found && skip < all[k]) {
+        const int holder = __ffs(__ballot_sync(0xffffffffu, skip < incl[k])) - 1;
+        skip -= __shfl_sync(0xffffffffu, incl[k] - n[k], holder);
+        start_r = k * 32 + holder;
+        found = true;
+      }
+      if (!found) skip -= all[k];
+    }
+  } else {                                                // a lane's requests follow each other
+    const int32_t per = (R + 31) / 32;
+    int64_t n = 0, incl;
+    for (int32_t r = lane * per; r < min((lane + 1) * per, R); ++r)
+      n += units_of(request<ROWS, TOKENS>(p, r, &bad));
+    U = scan(n, incl);
+    if (bad && blockIdx.x == 0) set_error(p.err, bad);
+    if (blockIdx.x >= U) return;
+    share();
+    int holder = __ffs(__ballot_sync(0xffffffffu, u_begin < incl)) - 1;
+    skip = u_begin - __shfl_sync(0xffffffffu, incl - n, holder);
+    start_r = holder * per;
+    const int32_t end = min(start_r + per, R);
+    for (int32_t base = start_r;; base += 32) {           // which of that lane's it is
+      Request q{};
+      if (base + lane < end) q = request<ROWS, TOKENS>(p, base + lane, &bad);
+      n = units_of(q);
+      const int64_t all = scan(n, incl);
+      if (skip < all || base + 32 >= end) {
+        const unsigned holds = __ballot_sync(0xffffffffu, skip < incl);
+        holder = holds ? __ffs(holds) - 1 : 31;
+        skip -= __shfl_sync(0xffffffffu, incl - n, holder);
+        start_r = base + holder;
+        break;
+      }
+      skip -= all;
+    }
   }
 
   Place fetch;                                            // what is loaded next
@@ -209,13 +248,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
     w.h = w.group = 0;
   };
   {
-    Request q;
-    q.n = __shfl_sync(0xffffffffu, mine.n, holder);
-    q.q0 = __shfl_sync(0xffffffffu, mine.q0, holder);
-    q.len = __shfl_sync(0xffffffffu, mine.len, holder);
-    q.groups = __shfl_sync(0xffffffffu, mine.groups, holder);
-    q.tile0 = __shfl_sync(0xffffffffu, mine.tile0, holder);
-    q.tiles = __shfl_sync(0xffffffffu, mine.tiles, holder);
+    const Request q = request<ROWS, TOKENS>(p, start_r, &bad);
     enter(fetch, start_r, q);
     if (skip < q.tiles) {                                 // (of the first head and group, mostly)
       fetch.tile += (int32_t)skip;
@@ -310,6 +343,31 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
   float o[HALVES][KS][NT][4];
   float mx[NT][2], sum[NT][2], qs[NT][2];
   int32_t top[NT][2], bottom[NT][2];                      // keys that a row sees: bottom .. top
+  // A place's queries as they are stored; a thread has row g of each eight, 4 of dim a k16 step.
+  const auto load_queries = [&](const Place& w) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = w.group * ROWS + nt * 8 + g;
+      const bool in = row < w.n * p.G;
+      const int i = in ? attend_query(p, row) : 0, j = in ? row - i * p.G : 0;
+      const uint16_t* src = p.q + (int64_t)(w.q0 + i) * p.q_token +
+                            (int64_t)(w.h * p.G + j) * p.q_head + c * (KS * 4);
+#pragma unroll
+      for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+        for (int k = 0; k < KS; k += 2) {
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (in)
+            v = p.q_vec ? __ldg(reinterpret_cast<const uint4*>(src + hf * 128 + k * 4))
+                        : attend_raw8(src + hf * 128 + k * 4);
+          qf[hf][k][nt][0] = v.x;
+          qf[hf][k][nt][1] = v.y;
+          qf[hf][k + 1][nt][0] = v.z;
+          qf[hf][k + 1][nt][1] = v.w;
+        }
+    }
+  };
+  load_queries(at);
   float v_ref = 0.0f;
   int stage = 0;
   bool fresh = true;
@@ -322,48 +380,39 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       v_ref = 1.17549435e-38f;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        const int row = at.group * ROWS + nt * 8 + g;
-        const bool in = row < at.n * p.G;
-        const int i = in ? row / p.G : 0, j = in ? row - i * p.G : 0;
-        const uint16_t* q = p.q + (int64_t)(at.q0 + i) * p.q_token + (int64_t)(at.h * p.G + j) * p.q_head;
-        float x[HALVES][KS][4];
         float big = 0.0f;
-#pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf) {
-          const uint16_t* src = q + hf * 128 + c * (KS * 4);
-#pragma unroll
-          for (int k = 0; k < KS; k += 2) {
-            float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (in) attend_load8(src + k * 4, p.q_vec, p.fp16, f);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              x[hf][k + (e >> 2)][e & 3] = f[e];
-              big = fmaxf(big, fabsf(f[e]));
-            }
-          }
-        }
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-        // a power of two of the row's size, kept where it and its inverse are normal
-        const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
-        const float by = __uint_as_float((254u - e) << 23);
 #pragma unroll
         for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            qf[hf][k][nt][0] = pack_half2(x[hf][k][0] * by, x[hf][k][1] * by);
-            qf[hf][k][nt][1] = pack_half2(x[hf][k][2] * by, x[hf][k][3] * by);
-          }
-        const float back = __uint_as_float(e << 23) * p.scale_log2;
+          for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int e2 = 0; e2 < 2; ++e2) {
-          qs[nt][e2] = __shfl_sync(0xffffffffu, back, (2 * c + e2) * 4);
-          mx[nt][e2] = -INFINITY;
-          sum[nt][e2] = 0.0f;
-          const int row2 = at.group * ROWS + nt * 8 + 2 * c + e2;
-          const int pos = at.len - at.n + row2 / p.G;
-          top[nt][e2] = p.causal ? min(pos, at.len - 1) : at.len - 1;
-          bottom[nt][e2] = p.window > 0 ? pos - p.window + 1 : 0;
+            for (int e = 0; e < 2; ++e) {
+              const float2 f = attend_unpack2(qf[hf][k][nt][e], p.fp16);
+              big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+            }
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        // a power of two of the row's size, kept where it and its inverse are normal
+        const uint32_t ex = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+        const float by = __uint_as_float((254u - ex) << 23);
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float2 f = attend_unpack2(qf[hf][k][nt][e], p.fp16);
+              qf[hf][k][nt][e] = pack_half2(f.x * by, f.y * by);
+            }
+        const float back = __uint_as_float(ex << 23) * p.scale_log2;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          qs[nt][e] = __shfl_sync(0xffffffffu, back, (2 * c + e) * 4);
+          mx[nt][e] = -INFINITY;
+          sum[nt][e] = 0.0f;
+          const int pos = at.len - at.n + attend_query(p, at.group * ROWS + nt * 8 + 2 * c + e);
+          top[nt][e] = p.causal ? min(pos, at.len - 1) : at.len - 1;
+          bottom[nt][e] = p.window > 0 ? pos - p.window + 1 : 0;
         }
       }
 #pragma unroll
@@ -548,7 +597,13 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       continue;
     }
 
-    // ---- the CTA's part of this (request, head, group) is done: its warps' results together
+    // ---- the CTA's part of this (request, head, group) is done: its warps' results together,
+    // while the next one's queries are on their way
+    const Place done = at;
+    if (u + 1 < units) {
+      step(at);
+      load_queries(at);
+    }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -598,17 +653,17 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       }
       __syncthreads();
     }
-    const bool all_of_it = seg_tile == at.tile0 && ends;
+    const bool all_of_it = seg_tile == done.tile0 && ends;
     // Output of rows by threads that hold values of dim 16 g + 2 k + {0, 1} (D = 64: 8 g + ...)
     const auto write = [&]() {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          const int row = at.group * ROWS + nt * 8 + 2 * c + e;
-          if (row >= at.n * p.G) continue;
-          const int i = row / p.G, j = row - i * p.G;
-          const int64_t r = (int64_t)(at.q0 + i) * (p.H * p.G) + at.h * p.G + j;
+          const int row = done.group * ROWS + nt * 8 + 2 * c + e;
+          if (row >= done.n * p.G) continue;
+          const int i = attend_query(p, row), j = row - i * p.G;
+          const int64_t r = (int64_t)(done.q0 + i) * (p.H * p.G) + done.h * p.G + j;
           const float l = sum[nt][e];
           const bool none = l == 0.0f;
           const float inv = none ? 0.0f : __fdividef(1.0f, l);
@@ -635,8 +690,8 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       // Partial results: the part that begins at this CTA's first unit in its slot 0, one that
       // begins later (and so runs past its last) in slot 1.  A slot is its rows' maxima, their
       // sums, and the sums of weighted values [row][dim].
-      const int64_t first = u_begin + u - (at.tile - at.tile0);       // units of the whole
-      const int64_t last = first + (at.tile_end - at.tile0) - 1;
+      const int64_t first = u_begin + u - (done.tile - done.tile0);       // units of the whole
+      const int64_t last = first + (done.tile_end - done.tile0) - 1;
       const int32_t c0 = (int32_t)(((first + 1) * E - 1) / U), c1 = (int32_t)(((last + 1) * E - 1) / U);
       constexpr int PS = ROWS * (D + 2);
       const int32_t odd = first > U * c0 / E ? 1 : 0;                 // the first part's slot
@@ -671,56 +726,71 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       if (last_s) {                                       // everyone else has left its part
         __threadfence();
         const int32_t parts = c1 - c0 + 1;
-        constexpr int UN = 10;                            // parts on their way at once
-        for (int f = tid; f < ROWS * D / 4; f += THREADS) {  // four values of a row
-          const int row = f / (D / 4);
-          const int full = at.group * ROWS + row;
-          if (full >= at.n * p.G) continue;
-          float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          float m = -INFINITY, l = 0.0f;
-          for (int32_t k0 = 0; k0 < parts; k0 += UN) {
-            float4 v[UN];
-            float pm[UN], pl[UN];
+        // A thread has NF times four values, THREADS apart; UN parts of them on their way at once.
+        constexpr int NF = (ROWS * D / 4 + THREADS - 1) / THREADS;
+        constexpr int UN = NF >= 4 ? 2 : NF >= 2 ? 4 : 10;
+        float4 acc[NF];
+        float m[NF], l[NF];
 #pragma unroll
-            for (int y = 0; y < UN; ++y) {
-              const bool in = k0 + y < parts;
-              const float* d = slot_of(in ? k0 + y : k0);
-              pm[y] = in ? __ldcg(d + row) : -INFINITY;
-              pl[y] = __ldcg(d + ROWS + row);
-              v[y] = __ldcg(reinterpret_cast<const float4*>(d + 2 * ROWS) + f);
-            }
-            float now = m;
+        for (int i = 0; i < NF; ++i) {
+          acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          m[i] = -INFINITY;
+          l[i] = 0.0f;
+        }
+        for (int32_t k0 = 0; k0 < parts; k0 += UN) {
+          float4 v[NF][UN];
+          float pm[NF][UN], pl[NF][UN];
 #pragma unroll
-            for (int y = 0; y < UN; ++y) now = fmaxf(now, pm[y]);
-            const float back = m == -INFINITY ? 0.0f : fast_exp2(m - now);
-            m = now;
-            l *= back;
-            acc.x *= back;
-            acc.y *= back;
-            acc.z *= back;
-            acc.w *= back;
+          for (int y = 0; y < UN; ++y) {
+            const bool in = k0 + y < parts;
+            const float* d = slot_of(in ? k0 + y : k0);
 #pragma unroll
-            for (int y = 0; y < UN; ++y) {
-              const float w = pm[y] == -INFINITY ? 0.0f : fast_exp2(pm[y] - m);
-              l = fmaf(w, pl[y], l);
-              acc.x = fmaf(w, v[y].x, acc.x);
-              acc.y = fmaf(w, v[y].y, acc.y);
-              acc.z = fmaf(w, v[y].z, acc.z);
-              acc.w = fmaf(w, v[y].w, acc.w);
+            for (int i = 0; i < NF; ++i) {
+              const int f = min(tid + i * THREADS, ROWS * D / 4 - 1), row = f / (D / 4);
+              pm[i][y] = in ? __ldcg(d + row) : -INFINITY;
+              pl[i][y] = __ldcg(d + ROWS + row);
+              v[i][y] = __ldcg(reinterpret_cast<const float4*>(d + 2 * ROWS) + f);
             }
           }
-          const int i = full / p.G, j = full - i * p.G;
-          const int64_t r = (int64_t)(at.q0 + i) * (p.H * p.G) + at.h * p.G + j;
-          const bool none = l == 0.0f;
-          const float inv = none ? 0.0f : __fdividef(1.0f, l);
+#pragma unroll
+          for (int i = 0; i < NF; ++i) {
+            float now = m[i];
+#pragma unroll
+            for (int y = 0; y < UN; ++y) now = fmaxf(now, pm[i][y]);
+            const float back = m[i] == -INFINITY ? 0.0f : fast_exp2(m[i] - now);
+            m[i] = now;
+            l[i] *= back;
+            acc[i].x *= back;
+            acc[i].y *= back;
+            acc[i].z *= back;
+            acc[i].w *= back;
+#pragma unroll
+            for (int y = 0; y < UN; ++y) {
+              const float w = pm[i][y] == -INFINITY ? 0.0f : fast_exp2(pm[i][y] - now);
+              l[i] = fmaf(w, pl[i][y], l[i]);
+              acc[i].x = fmaf(w, v[i][y].x, acc[i].x);
+              acc[i].y = fmaf(w, v[i][y].y, acc[i].y);
+              acc[i].z = fmaf(w, v[i][y].z, acc[i].z);
+              acc[i].w = fmaf(w, v[i][y].w, acc[i].w);
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NF; ++i) {
+          const int f = tid + i * THREADS, row = f / (D / 4), full = done.group * ROWS + row;
+          if (f >= ROWS * D / 4 || full >= done.n * p.G) continue;
+          const int a = attend_query(p, full), b = full - a * p.G;
+          const int64_t r = (int64_t)(done.q0 + a) * (p.H * p.G) + done.h * p.G + b;
+          const bool none = l[i] == 0.0f;
+          const float inv = none ? 0.0f : __fdividef(1.0f, l[i]);
           uint2 w = make_uint2(0u, 0u);
           if (!none) {
-            w.x = attend_pack2(p.fp16, acc.x * inv, acc.y * inv);
-            w.y = attend_pack2(p.fp16, acc.z * inv, acc.w * inv);
+            w.x = attend_pack2(p.fp16, acc[i].x * inv, acc[i].y * inv);
+            w.y = attend_pack2(p.fp16, acc[i].z * inv, acc[i].w * inv);
           }
           *reinterpret_cast<uint2*>(p.out + r * D + (f - row * (D / 4)) * 4) = w;
           if (f == row * (D / 4) && p.lse)
-            p.lse[r] = none ? -INFINITY : (m - kShift + log2f(l)) * 0.69314718055994531f;
+            p.lse[r] = none ? -INFINITY : (m[i] - kShift + log2f(l[i])) * 0.69314718055994531f;
         }
         __syncthreads();
         if (tid == 0) p.counters[c0] = 0;                 // as the next call finds it
@@ -728,7 +798,6 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       __syncthreads();
     }
     fresh = true;
-    if (u + 1 < units) step(at);
   }
   if (bad) set_error(p.err, bad);
 }

@@ -16,6 +16,7 @@ struct AttendParams {
   int32_t n_blocks;
   int32_t H;                 // kv heads
   int32_t G;                 // query heads of each
+  uint32_t G_inv;            // ceil(2^32 / G), or 0: see attend_query
   int32_t bt_log2;
   const uint16_t* q;
   int64_t q_token, q_head;   // strides, in elements
@@ -69,6 +70,12 @@ __device__ __forceinline__ bool attend_request(const AttendParams& p, int32_t r,
   return true;
 }
 
+// The query that a request's row belongs to: row / G.  With m = ceil(2^32 / G), m * G is less than
+// G over 2^32, so row * m / 2^32 is exact while row * G < 2^32; the host gives m where every row is.
+__device__ __forceinline__ int32_t attend_query(const AttendParams& p, int32_t row) {
+  return p.G_inv ? (int32_t)__umulhi((uint32_t)row, p.G_inv) : row / p.G;
+}
+
 // 8 values of 16 bits that are only 2-byte aligned
 __device__ __forceinline__ uint4 attend_raw8(const uint16_t* src) {
   uint32_t w[4];
@@ -78,25 +85,19 @@ __device__ __forceinline__ uint4 attend_raw8(const uint16_t* src) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+__device__ __forceinline__ float2 attend_unpack2(uint32_t w, int fp16) {
+  if (fp16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
 __device__ __forceinline__ void attend_unpack8(const uint4& v, int fp16, float (&f)[8]) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    if (fp16) {
-      const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-      f[2 * i] = t.x;
-      f[2 * i + 1] = t.y;
-    } else {
-      f[2 * i] = __uint_as_float(w[i] << 16);
-      f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    const float2 t = attend_unpack2(w[i], fp16);
+    f[2 * i] = t.x;
+    f[2 * i + 1] = t.y;
   }
-}
-
-// 8 values of 16 bits as floats
-__device__ __forceinline__ void attend_load8(const uint16_t* src, int vec, int fp16,
-                                             float (&f)[8]) {
-  attend_unpack8(vec ? __ldg(reinterpret_cast<const uint4*>(src)) : attend_raw8(src), fp16, f);
 }
 
 // 2^x to 2 units in the last place; below the normal range 0

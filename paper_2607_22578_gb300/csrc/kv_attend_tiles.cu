@@ -297,10 +297,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         it.rows0 = max(pairs - 1 - x / p.H, 0) * kPairRows;
         const int32_t before_q = it.len - it.n;     // the first query's position
         if (p.window > 0)
-          it.tile0 = max(0, before_q + it.rows0 / p.G - p.window + 1) / kTileTokens;
+          it.tile0 = max(0, before_q + attend_query(p, it.rows0) - p.window + 1) / kTileTokens;
         const auto steps = [&](int32_t first) {     // of the tile of rows that begins there
           if (first >= it.rows) return 0;
-          const int32_t i1 = min(it.n - 1, (first + kTileRows - 1) / p.G);
+          const int32_t i1 = min(it.n - 1, attend_query(p, first + kTileRows - 1));
           const int32_t see = p.causal ? min(it.len, before_q + i1 + 1) : it.len;
           // (where nothing is seen: one, hidden)
           return max(1, (see + kTileTokens - 1) / kTileTokens - it.tile0);
@@ -536,7 +536,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     Item it{}, next{};
     uint4 qv[NQ / 2];                               // half of them at a time
     const auto output_row = [&](const Item& w, int32_t full) {
-      const int32_t i = full / p.G, j = full - i * p.G;
+      const int32_t i = attend_query(p, full), j = full - i * p.G;
       return (int64_t)(w.q0 + i) * (p.H * p.G) + w.h * p.G + j;
     };
     // The next item with rows of this tile's, if it has been said: the items up to it may have to
@@ -566,7 +566,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             next.rows0 + x * kTileRows + (warp & 3) * 32 + (i0 + i) * RS + lane / LR;
         qv[i] = make_uint4(0u, 0u, 0u, 0u);
         if (next.more && full < next.rows) {
-          const int32_t a = full / p.G, b = full - a * p.G;
+          const int32_t a = attend_query(p, full), b = full - a * p.G;
           const uint16_t* src = p.q + (int64_t)(next.q0 + a) * p.q_token +
                                 (int64_t)(next.h * p.G + b) * p.q_head + (lane % LR) * 8;
           qv[i] = p.q_vec ? __ldg(reinterpret_cast<const uint4*>(src)) : attend_raw8(src);
@@ -612,12 +612,12 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       qs = qs_next;
       const int32_t n_steps = x ? it.steps1 : it.steps0;
       const int32_t rows0 = it.rows0 + x * kTileRows;
-      const int32_t pos = it.len - it.n + min(rows0 + row, it.rows - 1) / p.G;
+      const int32_t pos = it.len - it.n + attend_query(p, min(rows0 + row, it.rows - 1));
       const int32_t top = p.causal ? min(pos, it.len - 1) : it.len - 1;
       const int32_t bottom = p.window > 0 ? pos - p.window + 1 : 0;
       // tokens that every row of the tile sees: from .. to
-      const int32_t pos0 = it.len - it.n + rows0 / p.G;
-      const int32_t pos1 = it.len - it.n + min(it.n - 1, (rows0 + kTileRows - 1) / p.G);
+      const int32_t pos0 = it.len - it.n + attend_query(p, rows0);
+      const int32_t pos1 = it.len - it.n + min(it.n - 1, attend_query(p, rows0 + kTileRows - 1));
       const int32_t to = p.causal ? min(pos0, it.len - 1) : it.len - 1;
       const int32_t from = p.window > 0 ? pos1 - p.window + 1 : 0;
       const uint32_t tile_base = tiles;
