@@ -635,9 +635,15 @@ class KvCache:
         self._at = ctypes.addressof(self._struct)
 
 
+# The checks of these calls read each attribute once: a property is 0.1 us of
+# host time, a small function's call 0.3, an allocation 1.5 (a view of one 1.7),
+# and a decoding step's kernels are 4 to 12 us.
+_I32 = torch.int32
+
+
 def _i32(t, name: str, n: int | None = None):
-    """t as a contiguous int32 CUDA tensor of n elements."""
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+    """The address of a contiguous int32 CUDA tensor of n elements."""
+    if t.dtype is not _I32 or not t.is_cuda or not t.is_contiguous():
         raise TypeError("%s must be a contiguous int32 CUDA tensor" % name)
     if n is not None and t.numel() != n:
         raise ValueError("%s must have %d elements" % (name, n))
@@ -660,20 +666,33 @@ def hs_kv_tables(have: torch.Tensor, fresh: torch.Tensor, table: torch.Tensor, p
     [n_req], cursor [2]), or writes them to ``out``; max_tokens is the number
     of new tokens, or more (slot -1 past them)."""
     n = have.numel()
-    if table.dim() != 2 or table.shape[0] != n:
+    at = table.shape
+    if len(at) != 2 or at[0] != n:
         raise ValueError("table must be [n_req, width]")
-    max_tokens = int(max_tokens)
+    if not (have.dtype is _I32 and fresh.dtype is _I32 and table.dtype is _I32
+            and pool.dtype is _I32 and have.is_cuda and fresh.is_cuda and table.is_cuda
+            and pool.is_cuda and have.is_contiguous() and fresh.is_contiguous()
+            and table.is_contiguous() and pool.is_contiguous()):
+        raise TypeError("have, fresh, table and pool must be contiguous int32 CUDA tensors")
+    if fresh.numel() != n:
+        raise ValueError("fresh must have %d elements" % n)
+    cp = _kv_cursor(cursor, "cursor")
     if out is None:
-        new = have.new_empty
-        out = (new(max_tokens), new(n + 1), new(n), cursor.new_empty(2))
-    slots, starts, lens, after = out
-    _check(load().hs_kv_tables(
-        _i32(have, "have"), _i32(fresh, "fresh", n), n,
-        None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"), int(block_tokens),
-        _i32(table, "table"), table.shape[1], _i32(pool, "pool"), pool.numel(),
-        _kv_cursor(cursor, "cursor"), _kv_cursor(after, "cursor out"),
-        _i32(starts, "starts", n + 1), _i32(lens, "lens", n), _i32(slots, "slots", max_tokens),
-        max_tokens, _stream(stream)))
+        dev = have.device
+        slots = torch.empty(max_tokens, dtype=_I32, device=dev)
+        starts = torch.empty(n + 1, dtype=_I32, device=dev)
+        lens = torch.empty_like(have)
+        after = torch.empty_like(cursor)
+        outs = (after.data_ptr(), starts.data_ptr(), lens.data_ptr(), slots.data_ptr())
+    else:
+        slots, starts, lens, after = out
+        outs = (_kv_cursor(after, "cursor out"), _i32(starts, "starts", n + 1),
+                _i32(lens, "lens", n), _i32(slots, "slots", max_tokens))
+    _check((_lib or load()).hs_kv_tables(
+        have.data_ptr(), fresh.data_ptr(), n,
+        None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"), block_tokens,
+        table.data_ptr(), at[1], pool.data_ptr(), pool.numel(), cp, *outs, max_tokens,
+        _stream(stream)))
     return slots, starts, lens, after
 
 
@@ -715,13 +734,14 @@ def hs_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     the cache's codes; block scales grow as they have to."""
     kp, dtype = _kv_heads(k, "k", cache.dim)
     vp, vtype = _kv_heads(v, "v", cache.dim)
-    T, H, _ = k.shape
-    if v.shape != k.shape or H != cache.n_kv_heads or vtype != dtype:
+    shape, by = k.shape, k.stride()
+    if v.shape != shape or shape[1] != cache.n_kv_heads or vtype != dtype:
         raise ValueError("k and v must both be [tokens, n_kv_heads, dim] of one dtype")
-    if v.stride() != k.stride():
+    if v.stride() != by:
         raise ValueError("k and v must have the same strides")
-    _check(load().hs_kv_append(cache._at, kp, vp, dtype, T, k.stride(0), k.stride(1),
-                               _i32(slots, "slots", T), _stream(stream)))
+    T = shape[0]
+    _check((_lib or load()).hs_kv_append(cache._at, kp, vp, dtype, T, by[0], by[1],
+                                         _i32(slots, "slots", T), _stream(stream)))
 
 
 def hs_kv_attend_workspace(cache: KvCache, n_heads: int, max_q: int) -> int:
@@ -740,39 +760,48 @@ def hs_kv_attend(cache: KvCache, q: torch.Tensor, lens: torch.Tensor, table: tor
     ``starts`` every request has tokens / n_req of them.  ``max_q`` is the
     most queries of a request (all of them, if it is not given).  Returns
     (out, shaped and typed like q, and lse float32 [tokens, n_heads])."""
-    qp, dtype = _kv_heads(q, "q", cache.dim)
-    T, heads, dim = q.shape
+    dtype = _KV_DTYPES.get(q.dtype)
+    shape, by = q.shape, q.stride()
+    if dtype is None or not q.is_cuda or len(shape) != 3 or shape[2] != cache.dim or by[2] != 1:
+        _kv_heads(q, "q", cache.dim)
+    T, heads, dim = shape
     n = lens.numel()
-    if table.dim() != 2 or table.shape[0] != n:
+    at = table.shape
+    if len(at) != 2 or at[0] != n:
         raise ValueError("table must be [n_req, width]")
+    if not (lens.dtype is _I32 and table.dtype is _I32 and lens.is_cuda and table.is_cuda
+            and lens.is_contiguous() and table.is_contiguous()):
+        raise TypeError("lens and table must be contiguous int32 CUDA tensors")
     if starts is None:
         if n and T % n:
             raise ValueError("without starts, every request has as many queries")
         each = T // n if n else 0
-        if max_q is not None and int(max_q) != each:
+        if max_q is not None and max_q != each:
             raise ValueError("max_q is not what every request has")
-        max_q = each
-    elif max_q is None:
-        max_q = T
+        max_q, sp = each, None
+    else:
+        sp = _i32(starts, "starts", n + 1)
+        if max_q is None:
+            max_q = T
     if out is None:
-        out = (torch.empty((T, heads, dim), dtype=q.dtype, device=q.device),
-               torch.empty((T, heads), dtype=torch.float32, device=q.device))
-    o, lse = out
-    if o.dtype != q.dtype or o.shape != q.shape or not o.is_cuda or not o.is_contiguous():
-        raise ValueError("out must be contiguous and like q")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2]
-                            or not lse.is_cuda or not lse.is_contiguous()):
-        raise ValueError("lse must be contiguous float32 [tokens, n_heads]")
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = torch.empty((T, heads), dtype=torch.float32, device=q.device)
+    else:
+        o, lse = out
+        if o.dtype != q.dtype or o.shape != shape or not o.is_cuda or not o.is_contiguous():
+            raise ValueError("out must be contiguous and like q")
+        if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2]
+                                or not lse.is_cuda or not lse.is_contiguous()):
+            raise ValueError("lse must be contiguous float32 [tokens, n_heads]")
     if workspace is None:
         workspace = torch.zeros(hs_kv_attend_workspace(cache, heads, max_q), dtype=torch.uint8,
                                 device=q.device)
-    _check(load().hs_kv_attend(
-        cache._at, qp, dtype, T, heads, q.stride(0), q.stride(1), _i32(lens, "lens"),
-        None if starts is None else _i32(starts, "starts", n + 1), n,
-        None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"), int(max_q),
-        _i32(table, "table"), table.shape[1], dim ** -0.5 if scale is None else scale,
-        int(causal), int(window), o.data_ptr(), None if lse is None else lse.data_ptr(),
-        workspace.data_ptr(), workspace.numel(), _stream(stream)))
+    _check((_lib or load()).hs_kv_attend(
+        cache._at, q.data_ptr(), dtype, T, heads, by[0], by[1], lens.data_ptr(), sp, n,
+        None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"), max_q, table.data_ptr(),
+        at[1], dim ** -0.5 if scale is None else scale, 1 if causal else 0, window, o.data_ptr(),
+        None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.nbytes,
+        _stream(stream)))
     return o, lse
 
 

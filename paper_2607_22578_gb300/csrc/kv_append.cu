@@ -323,7 +323,7 @@ hs_status launch(const AppendParams& p, bool vec, dim3 grid, cudaStream_t stream
 template <int FMT, bool FP16>
 hs_status launch_pieces(const AppendParams& p, bool vec, dim3 grid, cudaStream_t stream) {
   const int pieces = (p.dim << p.bt_log2) / 8;  // of a block: 128 to 4096
-  if (pieces <= 128 * 4) return launch<FMT, FP16, 128, 4>(p, vec, grid, stream);
+  if (pieces <= 64 * 8) return launch<FMT, FP16, 64, 8>(p, vec, grid, stream);
   if (pieces <= 128 * 8) return launch<FMT, FP16, 128, 8>(p, vec, grid, stream);
   if (pieces <= 128 * 16) return launch<FMT, FP16, 128, 16>(p, vec, grid, stream);
   return launch<FMT, FP16, 256, 16>(p, vec, grid, stream);
