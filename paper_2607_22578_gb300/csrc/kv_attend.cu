@@ -63,11 +63,6 @@ __device__ __forceinline__ uint32_t chunk_at(int r, int c) {
     return (uint32_t)(r * D + (c & ~7) * 16 + (((c ^ r) & 7) << 4));
 }
 
-__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, bool in) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-               "r"(in ? 16 : 0)
-               : "memory");
-}
 __device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void* src, bool in) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src),
                "r"(in ? 4 : 0)

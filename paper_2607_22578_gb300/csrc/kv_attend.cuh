@@ -100,6 +100,13 @@ __device__ __forceinline__ void attend_unpack8(const uint4& v, int fp16, float (
   }
 }
 
+// cp.async of 16 bytes, or of as many zeros
+__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void* src, bool in) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+               "r"(in ? 16 : 0)
+               : "memory");
+}
+
 // 2^x to 2 units in the last place; below the normal range 0
 __device__ __forceinline__ float fast_exp2(float x) {
   float y;

@@ -531,10 +531,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     uint32_t items = 0, tiles = 0, ns = 0;          // of the CTA; steps of this tile of rows
     bool ok = true;
 
-    // Queries: D / 8 lanes a row, 8 values each, so that a load is of whole rows.
+    // Queries: D / 8 lanes a row, 8 values each, so that a load is of whole rows.  They are copied to
+    // their place as they are, while the last step's scores become weights, and become half there.
     constexpr int LR = D / 8, RS = 32 / LR, NQ = 32 / RS;  // lanes of a row, rows of a load, loads
     Item it{}, next{};
-    uint4 qv[NQ / 2];                               // half of them at a time
     const auto output_row = [&](const Item& w, int32_t full) {
       const int32_t i = attend_query(p, full), j = full - i * p.G;
       return (int64_t)(w.q0 + i) * (p.H * p.G) + w.h * p.G + j;
@@ -559,26 +559,36 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         tiles += next.tiles;
       }
     };
-    const auto fetch = [&](int i0) {                // its queries, on their way
-#pragma unroll
-      for (int i = 0; i < NQ / 2; ++i) {
-        const int32_t full =
-            next.rows0 + x * kTileRows + (warp & 3) * 32 + (i0 + i) * RS + lane / LR;
-        qv[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (next.more && full < next.rows) {
-          const int32_t a = attend_query(p, full), b = full - a * p.G;
-          const uint16_t* src = p.q + (int64_t)(next.q0 + a) * p.q_token +
-                                (int64_t)(next.h * p.G + b) * p.q_head + (lane % LR) * 8;
-          qv[i] = p.q_vec ? __ldg(reinterpret_cast<const uint4*>(src)) : attend_raw8(src);
+    const int q_row = (warp & 3) * 32 + lane / LR, q_chunk = lane % LR;  // of this thread's first load
+    const uint32_t q_line = base + L::kQ + x * L::kTileBytes + (q_chunk >> 3) * L::kBlockBytes;
+    const auto q_place = [&](int i) {
+      const int r = q_row + i * RS;
+      return q_line + r * 128 + (((q_chunk ^ r) & 7) << 4);
+    };
+    const auto fetch = [&]() {
+      const int32_t first = next.rows0 + x * kTileRows + q_row;
+      const uint16_t* heads = p.q + (int64_t)next.h * p.G * p.q_head + q_chunk * 8;
+#pragma unroll 4
+      for (int i = 0; i < NQ; ++i) {
+        const int32_t full = first + i * RS;
+        const bool in = full < next.rows;
+        const int32_t a = in ? attend_query(p, full) : 0, b = in ? full - a * p.G : 0;
+        const uint16_t* src = heads + (int64_t)(next.q0 + a) * p.q_token + (int64_t)b * p.q_head;
+        if (p.q_vec) {
+          cp_async16_zfill(q_place(i), src, in);
+        } else {
+          const uint4 v = in ? attend_raw8(src) : make_uint4(0u, 0u, 0u, 0u);
+          sts128(q_place(i), v.x, v.y, v.z, v.w);
         }
       }
     };
-    float qs = 0.0f, qs_next = 0.0f;
-    const auto put = [&](int i0) {                  // and into place: the last scores are there
-#pragma unroll
-      for (int i = 0; i < NQ / 2; ++i) {
+    float qs = 0.0f;
+    const auto put = [&]() {
+      cp_async_wait_all();
+#pragma unroll 2
+      for (int i = 0; i < NQ; ++i) {
         float f[8], big = 0.0f;
-        attend_unpack8(qv[i], p.fp16, f);
+        attend_unpack8(lds128(q_place(i)), p.fp16, f);
 #pragma unroll
         for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(f[e]));
 #pragma unroll
@@ -586,30 +596,71 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         // a power of two of the row's size, kept where it and its inverse are normal
         const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
         const float by = __uint_as_float((254u - e) << 23);
-        const int r = (warp & 3) * 32 + (i0 + i) * RS + lane / LR, ch = lane % LR;
-        sts128(base + L::kQ + x * L::kTileBytes + (ch >> 3) * L::kBlockBytes + r * 128 +
-                   (((ch ^ r) & 7) << 4),
-               half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
+        sts128(q_place(i), half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
                half2_of(f[4] * by, f[5] * by), half2_of(f[6] * by, f[7] * by));
         const uint32_t mine = __shfl_sync(0xffffffffu, e, (lane % RS) * LR);
-        if (lane / RS == i0 + i) qs_next = __uint_as_float(mine << 23) * p.scale_log2;
+        if (lane / RS == i) qs = __uint_as_float(mine << 23) * p.scale_log2;
       }
-    };
-    const auto put_all = [&]() {                    // the first half was fetched
-      put(0);
-      fetch(NQ / 2);
-      put(NQ / 2);
       fence_async_shared();
       mbar_arrive(&sh.q_full[x]);
     };
-    bool known = take(true);
-    if (ok && next.more) {
-      fetch(0);
-      put_all();
-    }
-    while (ok && next.more) {
+    bool known = false, started = false;
+    float m = -INFINITY, sum = 0.0f;
+    for (;;) {
+      if (!known) {
+        if (!take(true)) break;
+        if (next.more) fetch();
+      }
+      if (next.more) put();
+
+      if (started) {
+        // ---- the output of the item before
+        const int32_t rows0 = it.rows0 + x * kTileRows;
+        const bool none = sum == 0.0f;
+        const float inv = none ? 0.0f : __fdividef(1.0f, sum);
+        if (p.lse && rows0 + row < it.rows)
+          p.lse[output_row(it, rows0 + row)] =
+              none ? -INFINITY : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
+        if (!(ok = wait(&sh.o_full[x][1], ns - 1))) break;
+        tc_fence_after();
+        // 32 of dim at a time through shared memory: a thread has a row, a store 64 bytes of eight
+        const uint32_t stage = base + L::kOut + warp * 2048;
+        uint16_t* dst[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int32_t full = rows0 + (warp & 3) * 32 + v * 8 + (lane >> 2);
+          dst[v] = full < it.rows ? p.out + output_row(it, full) * D + (lane & 3) * 8 : nullptr;
+        }
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld_32x32b_x32(t_o + c * 32, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = none ? 0u
+                          : attend_pack2(p.fp16, __uint_as_float(o[v * 8 + 2 * e]) * inv,
+                                         __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
+            sts128(stage + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
+          }
+          __syncwarp();
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int r = v * 8 + (lane >> 2);
+            const uint4 y = lds128(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+            if (dst[v]) *reinterpret_cast<uint4*>(dst[v] + c * 32) = y;
+          }
+          __syncwarp();
+        }
+        tc_fence_before();
+      }
+      if (!next.more) break;
       it = next;
-      qs = qs_next;
+      started = true;
+      known = false;
       const int32_t n_steps = x ? it.steps1 : it.steps0;
       const int32_t rows0 = it.rows0 + x * kTileRows;
       const int32_t pos = it.len - it.n + attend_query(p, min(rows0 + row, it.rows - 1));
@@ -623,10 +674,15 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       const uint32_t tile_base = tiles;
       tiles += it.tiles;
 
-      float m = -INFINITY, sum = 0.0f;
+      m = -INFINITY;
+      sum = 0.0f;
       for (int32_t u = 0; u < n_steps; ++u, ++ns) {
         if (!(ok = wait(&sh.s_full[x], ns))) break;
         tc_fence_after();
+        if (u + 1 == n_steps) {                       // the last product to read the queries is done
+          known = take(false);
+          if (known && next.more) fetch();
+        }
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
           const float4* scales =
@@ -720,58 +776,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         if (!ok) break;
       }
       if (!ok) break;
-
-      // ---- the output, after the next item's queries
-      known = take(false);
-      if (known && next.more) {
-        fetch(0);
-        put_all();
-      }
-      const bool none = sum == 0.0f;
-      const float inv = none ? 0.0f : __fdividef(1.0f, sum);
-      if (p.lse && rows0 + row < it.rows)
-        p.lse[output_row(it, rows0 + row)] =
-            none ? -INFINITY : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
-      if (!(ok = wait(&sh.o_full[x][1], ns - 1))) break;
-      tc_fence_after();
-      // 32 of dim at a time through shared memory: a thread has a row, a store 64 bytes of eight
-      const uint32_t stage = base + L::kOut + warp * 2048;
-      uint16_t* dst[4];
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int32_t full = rows0 + (warp & 3) * 32 + v * 8 + (lane >> 2);
-        dst[v] = full < it.rows ? p.out + output_row(it, full) * D + (lane & 3) * 8 : nullptr;
-      }
-#pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        tmem_ld_32x32b_x32(t_o + c * 32, o);
-        tmem_ld_wait();
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            w[e] = none ? 0u
-                        : attend_pack2(p.fp16, __uint_as_float(o[v * 8 + 2 * e]) * inv,
-                                       __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
-          sts128(stage + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int r = v * 8 + (lane >> 2);
-          const uint4 y = lds128(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
-          if (dst[v]) *reinterpret_cast<uint4*>(dst[v] + c * 32) = y;
-        }
-        __syncwarp();
-      }
-      tc_fence_before();
-      if (!known && take(true) && next.more) {
-        fetch(0);
-        put_all();
-      }
     }
+    cp_async_wait_all();
   }
   tc_fence_before();
   __syncthreads();
