@@ -51,7 +51,7 @@ constexpr int attend_ctas() {
 }
 
 template <int D>
-constexpr int stage_bytes() { return 2 * kWarpTokens * D + 16; }  // K, V, two scales of each
+constexpr int stage_bytes() { return 2 * kWarpTokens * D + 128; }  // K, V, two scales of each
 
 // Where 16-byte chunk c of token row r of a tile lies, so that both ways of reading it (8 tokens
 // by 2 chunks, 4 even tokens by 2 chunks) touch every bank once.
@@ -102,25 +102,36 @@ struct Place {
   int32_t n, q0, len;
 };
 
+// The instruction cache is small beside this kernel, and what runs once a request or once a launch
+// would push out what runs for every tile: such code stands out of line, or once in a loop.
+__device__ __noinline__ int64_t quotient_64(int64_t a, int64_t b) { return a / b; }
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {  // of numbers >= 0
+  return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : quotient_64(a, b);
+}
+
+// What a request with n queries over len tokens asks for, in groups of ROWS rows and tiles of TOKENS
+// tokens; groups = 0 if nothing, or if it is another kernel's.
 struct Request {
-  int32_t n, q0, len, groups, tile0, tiles;  // tiles of a CTA's tokens
+  int32_t n, q0, len, groups, tile0, tiles;
+  int32_t bad;
 };
 
-// What request r asks for; groups = 0 if nothing (or nothing that can be done: *bad).
 template <int ROWS, int TOKENS>
-__device__ __forceinline__ Request request(const AttendParams& p, int32_t r, unsigned* bad) {
-  Request q;
-  q.groups = 0;
-  q.tile0 = 0;
-  q.tiles = 0;
-  if (!attend_request(p, r, q.n, q.q0, q.len, bad)) return q;
-  if (q.n * p.G > p.rows_most) return q;                // another kernel's
+__device__ __forceinline__ void divide(const AttendParams& p, Request& q) {
+  q.groups = q.tile0 = q.tiles = 0;
+  if (q.n == 0 || q.n * p.G > p.rows_most) return;
   q.groups = (q.n * p.G + ROWS - 1) / ROWS;
-  if (p.window > 0) {
-    const int32_t first = q.len - q.n - p.window + 1;
-    if (first > 0) q.tile0 = first / TOKENS;
-  }
+  if (p.window > 0) q.tile0 = max(q.len - q.n - p.window + 1, 0) / TOKENS;
   q.tiles = max((q.len + TOKENS - 1) / TOKENS - q.tile0, 1);  // an empty one too
+}
+
+template <int ROWS, int TOKENS>
+__device__ __noinline__ Request request(const AttendParams& p, int32_t r) {
+  Request q{};
+  unsigned bad = 0;
+  if (!attend_request(p, r, q.n, q.q0, q.len, &bad)) q.n = 0;
+  q.bad = (int32_t)bad;
+  divide<ROWS, TOKENS>(p, q);
   return q;
 }
 
@@ -143,16 +154,17 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
   float* merge = reinterpret_cast<float*>(smem + WARPS * kAttStages * stage_bytes<D>());
   const uint32_t ring_u = smem_u32(ring);
 
-  pdl_wait();
+  // Beside the kernel of the requests with many rows nothing is waited for: that one has seen to it
+  // that what came before is done, and shares no output or workspace with this one.
+  if (!p.apart) pdl_wait();
   pdl_trigger();
   const int32_t R = p.n_req_dev ? max(0, min(__ldg(p.n_req_dev), p.n_req)) : p.n_req;
 
   // ---- how many units there are, and which are this CTA's: each warp for itself, so that no
   // barrier stands before the first loads
-  unsigned bad = 0;
+  int32_t bad = 0;
   const auto units_of = [&](const Request& q) { return (int64_t)q.groups * q.tiles * p.H; };
-  // Of lanes' consecutive counts x: the total, and for the lane that holds number `at` of them the
-  // count before its own.
+  // Of lanes' counts x: up to and with each lane, and all
   const auto scan = [&](int64_t x, int64_t& incl) {
     incl = x;
 #pragma unroll
@@ -162,35 +174,53 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
     }
     return __shfl_sync(0xffffffffu, incl, 31);
   };
-  int64_t U, u_begin, u_end, E, skip;
-  int32_t start_r;
-  const auto share = [&]() {                              // of U units
-    E = min((int64_t)gridDim.x, U);                       // CTAs with work
-    u_begin = U * blockIdx.x / E;
-    u_end = U * (blockIdx.x + 1) / E;
-  };
   constexpr int CHUNKS = 4;
-  if (R <= 32 * CHUNKS) {                                 // a lane's requests are 32 apart
-    int64_t n[CHUNKS], incl[CHUNKS], all[CHUNKS];
+  const bool few = R <= 32 * CHUNKS;
+  int64_t n[CHUNKS] = {}, incl[CHUNKS] = {}, all[CHUNKS] = {};
+  const int32_t per = (R + 31) / 32;
+  Request q[CHUNKS];
+  if (few) {                                              // a lane's requests are 32 apart
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-      Request q{};
-      if (k * 32 + lane < R) q = request<ROWS, TOKENS>(p, k * 32 + lane, &bad);
-      n[k] = units_of(q);
+      unsigned b = 0;
+      q[k] = Request{};
+      if (k * 32 + lane < R && !attend_request(p, k * 32 + lane, q[k].n, q[k].q0, q[k].len, &b))
+        q[k].n = 0;
+      bad |= (int32_t)b;
     }
-    U = 0;
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
-      all[k] = 0;
-      incl[k] = 0;
+      divide<ROWS, TOKENS>(p, q[k]);
+      n[k] = units_of(q[k]);
       if (k * 32 < R) all[k] = scan(n[k], incl[k]);
-      U += all[k];
     }
-    if (bad && blockIdx.x == 0) set_error(p.err, bad);
-    if (blockIdx.x >= U) return;
-    share();
-    skip = u_begin;
-    start_r = 0;
+  } else {                                                // they follow each other
+#pragma unroll 1
+    for (int32_t r = lane * per; r < min((lane + 1) * per, R); ++r) {
+      const Request q = request<ROWS, TOKENS>(p, r);
+      bad |= q.bad;
+      n[0] += units_of(q);
+    }
+    all[0] = scan(n[0], incl[0]);
+  }
+  const int64_t U = all[0] + all[1] + all[2] + all[3];
+  if (bad && blockIdx.x == 0) set_error(p.err, (unsigned)bad);
+  if (blockIdx.x >= U) {
+    if (p.apart) pdl_wait();
+    return;
+  }
+  const int64_t E = min((int64_t)gridDim.x, U);           // CTAs with work: share units each, and
+  const int64_t share = quotient(U, E), longer = U - share * E;  // the first `longer` one more
+  const auto begins = [&](int64_t cta) { return cta * share + min(cta, longer); };
+  const auto cta_of = [&](int64_t u) {
+    const int64_t cut = longer * (share + 1);
+    return (int32_t)(u < cut ? quotient(u, share + 1) : longer + quotient(u - cut, share));
+  };
+  const int64_t u_begin = begins(blockIdx.x), units = begins(blockIdx.x + 1) - u_begin;
+  int64_t skip = u_begin;                                 // units before its first in start_r
+  int32_t start_r = 0;
+  Request start{};
+  if (few) {
     bool found = false;
 #pragma unroll
     for (int k = 0; k < CHUNKS; ++k) {
@@ -198,80 +228,58 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
         const int holder = __ffs(__ballot_sync(0xffffffffu, skip < incl[k])) - 1;
         skip -= __shfl_sync(0xffffffffu, incl[k] - n[k], holder);
         start_r = k * 32 + holder;
+        start.n = __shfl_sync(0xffffffffu, q[k].n, holder);
+        start.q0 = __shfl_sync(0xffffffffu, q[k].q0, holder);
+        start.len = __shfl_sync(0xffffffffu, q[k].len, holder);
         found = true;
       }
       if (!found) skip -= all[k];
     }
-  } else {                                                // a lane's requests follow each other
-    const int32_t per = (R + 31) / 32;
-    int64_t n = 0, incl;
-    for (int32_t r = lane * per; r < min((lane + 1) * per, R); ++r)
-      n += units_of(request<ROWS, TOKENS>(p, r, &bad));
-    U = scan(n, incl);
-    if (bad && blockIdx.x == 0) set_error(p.err, bad);
-    if (blockIdx.x >= U) return;
-    share();
-    int holder = __ffs(__ballot_sync(0xffffffffu, u_begin < incl)) - 1;
-    skip = u_begin - __shfl_sync(0xffffffffu, incl - n, holder);
+    divide<ROWS, TOKENS>(p, start);
+  } else {
+    int holder = __ffs(__ballot_sync(0xffffffffu, skip < incl[0])) - 1;
+    skip -= __shfl_sync(0xffffffffu, incl[0] - n[0], holder);
     start_r = holder * per;
     const int32_t end = min(start_r + per, R);
+#pragma unroll 1
     for (int32_t base = start_r;; base += 32) {           // which of that lane's it is
-      Request q{};
-      if (base + lane < end) q = request<ROWS, TOKENS>(p, base + lane, &bad);
-      n = units_of(q);
-      const int64_t all = scan(n, incl);
-      if (skip < all || base + 32 >= end) {
-        const unsigned holds = __ballot_sync(0xffffffffu, skip < incl);
+      int64_t one = 0, upto;
+      if (base + lane < end) one = units_of(request<ROWS, TOKENS>(p, base + lane));
+      const int64_t some = scan(one, upto);
+      if (skip < some || base + 32 >= end) {
+        const unsigned holds = __ballot_sync(0xffffffffu, skip < upto);
         holder = holds ? __ffs(holds) - 1 : 31;
-        skip -= __shfl_sync(0xffffffffu, incl - n, holder);
+        skip -= __shfl_sync(0xffffffffu, upto - one, holder);
         start_r = base + holder;
         break;
       }
-      skip -= all;
+      skip -= some;
     }
+    start = request<ROWS, TOKENS>(p, start_r);
   }
 
-  Place fetch;                                            // what is loaded next
-  const auto enter = [&](Place& w, int32_t r, const Request& q) {
-    w.r = r;
-    w.groups = q.groups;
-    w.n = q.n;
-    w.q0 = q.q0;
-    w.len = q.len;
-    w.tile0 = w.tile = q.tile0;
-    w.tile_end = q.tile0 + q.tiles;
-    w.h = w.group = 0;
+  Place fetch{};                                          // what is loaded next
+  const auto enter = [&](int32_t r, const Request& w) {
+    fetch.r = r;
+    fetch.groups = w.groups;
+    fetch.n = w.n;
+    fetch.q0 = w.q0;
+    fetch.len = w.len;
+    fetch.tile0 = fetch.tile = w.tile0;
+    fetch.tile_end = w.tile0 + w.tiles;
+    fetch.h = fetch.group = 0;
   };
-  {
-    const Request q = request<ROWS, TOKENS>(p, start_r, &bad);
-    enter(fetch, start_r, q);
-    if (skip < q.tiles) {                                 // (of the first head and group, mostly)
-      fetch.tile += (int32_t)skip;
-    } else {
-      const int64_t part = skip / q.tiles;                // which (head, group)
-      fetch.tile += (int32_t)(skip - part * q.tiles);
-      fetch.h = (int32_t)(part / q.groups);
-      fetch.group = (int32_t)(part - (int64_t)fetch.h * q.groups);
-    }
-  }
-  const auto open = [&](Place& w, int32_t r) {            // the next request with work
-    Request q{0, 0, 0, 1, 0, 1};                          // (of none, should the lengths change)
+  const auto open = [&](int32_t r) {                      // ... the next request with work
+    Request w{0, 0, 0, 1, 0, 1, 0};                       // (of none, should the lengths change)
+#pragma unroll 1
     for (; r < R; ++r) {
-      const Request x = request<ROWS, TOKENS>(p, r, &bad);
+      const Request x = request<ROWS, TOKENS>(p, r);
       if (x.groups > 0) {
-        q = x;
+        w = x;
         break;
       }
     }
-    enter(w, r, q);
-  };
-  const auto step = [&](Place& w) {                       // to the next unit of the list
-    if (++w.tile < w.tile_end) return;
-    w.tile = w.tile0;
-    if (++w.group < w.groups) return;
-    w.group = 0;
-    if (++w.h < p.H) return;
-    open(w, w.r + 1);
+    enter(r, w);
   };
 
   // ---- loading: this warp's 32 tokens of a unit, one stage
@@ -295,15 +303,21 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       const int64_t in = (int64_t)(t0 & ((1 << p.bt_log2) - 1)) * D;
       const int64_t b0 = ((((int64_t)id0 * p.H + fetch.h) << p.bt_log2) * D) + in;
       const int64_t b1 = two ? (((int64_t)id1 * p.H + fetch.h) << 4) * D - 16 * D : b0;
-      constexpr int CH = D / 16;                          // chunks of a row
+      // A lane's copies are RPI rows, 512 bytes, apart, from its own place in the first rows on;
+      // rows past the end are zeros (their addresses are inside the block all the same).
+      constexpr int CH = D / 16, RPI = 32 / CH;           // chunks of a row, rows of a copy
+      const int r0 = lane / CH;
+      const uint8_t* k0 = p.k + b0 + lane * 16;
+      const uint8_t* v0 = p.v + b0 + lane * 16;
+      const int64_t other = b1 - b0;                      // of the second 16 tokens
+      const uint32_t dst = base + chunk_at<D>(r0, lane % CH);
 #pragma unroll
-      for (int i = 0; i < kWarpTokens * CH / 32; ++i) {
-        const int at = i * 32 + lane, r = at / CH, ch = at % CH;
-        const int64_t off = (r < 16 ? b0 : b1) + r * D + ch * 16;
-        const bool ok = r < left;
-        const uint32_t dst = base + chunk_at<D>(r, ch);
-        cp_async16_zfill(dst, p.k + (ok ? off : 0), ok);
-        cp_async16_zfill(dst + kWarpTokens * D, p.v + (ok ? off : 0), ok);
+      for (int i = 0; i < CH; ++i) {
+        const bool ok = r0 < left - i * RPI;
+        const int64_t off = i * 512 + (i < CH / 2 ? 0 : other);
+        const uint32_t to = (dst + i * 512) ^ (D == 64 ? 0 : ((i * RPI) & 7) << 4);
+        cp_async16_zfill(to, k0 + off, ok);
+        cp_async16_zfill(to + kWarpTokens * D, v0 + off, ok);
       }
       if (lane < 4) {
         const float* s = lane < 2 ? p.ks : p.vs;
@@ -317,22 +331,6 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
                      : "memory");
     }
   };
-
-  const int64_t units = u_end - u_begin;
-  int64_t fetched = 0;
-  look_up();
-  Place at = fetch;                                       // what is computed next
-#pragma unroll
-  for (int s = 0; s < kAttStages - 1; ++s) {
-    if (fetched < units) {
-      load(s);
-      if (++fetched < units) {
-        step(fetch);
-        look_up();
-      }
-    }
-    cp_async_commit();
-  }
 
   uint32_t qf[HALVES][KS][NT][2];
   float o[HALVES][KS][NT][4];
@@ -351,7 +349,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
         for (int k = 0; k < KS; k += 2) {
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);  // (unaligned rows: a call)
           if (in)
             v = p.q_vec ? __ldg(reinterpret_cast<const uint4*>(src + hf * 128 + k * 4))
                         : attend_raw8(src + hf * 128 + k * 4);
@@ -362,243 +360,264 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
         }
     }
   };
-  load_queries(at);
+  // Where in a tile this thread's keys (row g of each eight) and values (rows 2c, 2c + 1) begin:
+  // the order of chunks repeats every eight rows.
+  uint32_t k_lane[(KS + 3) / 4], v_lane[2];
+#pragma unroll
+  for (int k = 0; k < (KS + 3) / 4; ++k) k_lane[k] = chunk_at<D>(g, (KS / 4) * c + k);
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+    v_lane[x] = D == 64 ? chunk_at<D>(2 * c + x, g >> 1) + (g & 1) * 8 : chunk_at<D>(2 * c + x, g);
   float v_ref = 0.0f;
-  int stage = 0;
   bool fresh = true;
   int32_t seg_tile = 0;                                   // the first tile that this CTA has of it
+  Place at{}, next{};                                     // what is computed, what was loaded last
 
-  for (int64_t u = 0; u < units; ++u) {
-    if (fresh) {                                          // a (request, head, group) begins
-      fresh = false;
-      seg_tile = at.tile;
-      v_ref = 1.17549435e-38f;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float big = 0.0f;
-#pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf)
-#pragma unroll
-          for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float2 f = attend_unpack2(qf[hf][k][nt][e], p.fp16);
-              big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
-            }
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
-        big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
-        // a power of two of the row's size, kept where it and its inverse are normal
-        const uint32_t ex = min(max(__float_as_uint(big) >> 23, 1u), 253u);
-        const float by = __uint_as_float((254u - ex) << 23);
-#pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf)
-#pragma unroll
-          for (int k = 0; k < KS; ++k)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float2 f = attend_unpack2(qf[hf][k][nt][e], p.fp16);
-              qf[hf][k][nt][e] = pack_half2(f.x * by, f.y * by);
-            }
-        const float back = __uint_as_float(ex << 23) * p.scale_log2;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          qs[nt][e] = __shfl_sync(0xffffffffu, back, (2 * c + e) * 4);
-          mx[nt][e] = -INFINITY;
-          sum[nt][e] = 0.0f;
-          const int pos = at.len - at.n + attend_query(p, at.group * ROWS + nt * 8 + 2 * c + e);
-          top[nt][e] = p.causal ? min(pos, at.len - 1) : at.len - 1;
-          bottom[nt][e] = p.window > 0 ? pos - p.window + 1 : 0;
+  enter(start_r, start);
+  if (skip < fetch.tile_end - fetch.tile0) {              // (of the first head and group, mostly)
+    fetch.tile += (int32_t)skip;
+  } else {
+    const int32_t tiles = fetch.tile_end - fetch.tile0;
+    const int64_t part = quotient(skip, tiles);           // which (head, group)
+    fetch.tile += (int32_t)(skip - part * tiles);
+    fetch.h = (int32_t)quotient(part, fetch.groups);
+    fetch.group = (int32_t)(part - (int64_t)fetch.h * fetch.groups);
+  }
+  look_up();
+#pragma unroll 1
+  for (int64_t i = 0; i <= units; ++i) {                  // load unit i, compute unit i - 1
+    __syncwarp();
+    if (i < units) {
+      load((int)(i & 1));
+      next = fetch;
+      if (i + 1 < units) {                                // the next unit of the list, and its blocks
+        if (++fetch.tile == fetch.tile_end) {
+          fetch.tile = fetch.tile0;
+          if (++fetch.group == fetch.groups) {
+            fetch.group = 0;
+            if (++fetch.h == p.H) open(fetch.r + 1);
+          }
         }
+        look_up();
       }
+    }
+    cp_async_commit();
+    bool ends = false;
+    if (i > 0) {
+      const int stage = (int)((i - 1) & 1);
+      if (fresh) {                                          // a (request, head, group) begins
+        fresh = false;
+        seg_tile = at.tile;
+        v_ref = 1.17549435e-38f;
 #pragma unroll
-      for (int hf = 0; hf < HALVES; ++hf)
+        for (int nt = 0; nt < NT; ++nt) {
+          float big = 0.0f;
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+          for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float2 f = attend_unpack2(qf[hf][k][nt][e], p.fp16);
+                big = fmaxf(big, fmaxf(fabsf(f.x), fabsf(f.y)));
+              }
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 1));
+          big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, 2));
+          // a power of two of the row's size, kept where it and its inverse are normal
+          const uint32_t ex = min(max(__float_as_uint(big) >> 23, 1u), 253u);
+          const float by = __uint_as_float((254u - ex) << 23);
+#pragma unroll
+          for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float2 f = attend_unpack2(qf[hf][k][nt][e], p.fp16);
+                qf[hf][k][nt][e] = pack_half2(f.x * by, f.y * by);
+              }
+          const float back = __uint_as_float(ex << 23) * p.scale_log2;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            qs[nt][e] = __shfl_sync(0xffffffffu, back, (2 * c + e) * 4);
+            mx[nt][e] = -INFINITY;
+            sum[nt][e] = 0.0f;
+            const int pos = at.len - at.n + attend_query(p, at.group * ROWS + nt * 8 + 2 * c + e);
+            top[nt][e] = p.causal ? min(pos, at.len - 1) : at.len - 1;
+            bottom[nt][e] = p.window > 0 ? pos - p.window + 1 : 0;
+          }
+        }
+#pragma unroll
+        for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[hf][k][nt][e] = 0.0f;
+      }
+
+      cp_async_wait<1>();
+      __syncwarp();
+      const uint32_t kb = ring_u + stage * stage_bytes<D>(), vb = kb + kWarpTokens * D;
+      float scales[4];
+      asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                   : "=f"(scales[0]), "=f"(scales[1]), "=f"(scales[2]), "=f"(scales[3])
+                   : "r"(kb + 2 * kWarpTokens * D)
+                   : "memory");
+      const int32_t t0 = at.tile * TOKENS + warp * kWarpTokens;
+      if (t0 < at.len) {
+        // ---- s = q . k: tokens are M, rows are N
+        float s[2][NT][4];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[hf][k][nt][e] = 0.0f;
-    }
-
-    cp_async_wait<kAttStages - 2>();
-    __syncwarp();
-    {  // the next load goes where the last unit was
-      const int s = stage == 0 ? kAttStages - 1 : stage - 1;
-      if (fetched < units) {
-        load(s);
-        if (++fetched < units) {
-          step(fetch);
-          look_up();
-        }
-      }
-      cp_async_commit();
-    }
-    const uint32_t kb = ring_u + stage * stage_bytes<D>(), vb = kb + kWarpTokens * D;
-    float scales[4];
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(scales[0]), "=f"(scales[1]), "=f"(scales[2]), "=f"(scales[3])
-                 : "r"(kb + 2 * kWarpTokens * D)
-                 : "memory");
-    const int32_t t0 = at.tile * TOKENS + warp * kWarpTokens;
-    if (t0 < at.len) {
-      // ---- s = q . k: tokens are M, rows are N
-      float s[2][NT][4];
+            for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.0f;
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[mt][nt][e] = 0.0f;
-#pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf) {
-          uint32_t a[2][KS];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int r = mt * 16 + x * 8 + g;
-#pragma unroll
-            for (int k = 0; k < KS; k += 4) {
-              const uint4 w = lds128(kb + chunk_at<D>(r, hf * 8 + (KS / 4) * c + k / 4));
-              a[x][k] = w.x;
-              a[x][k + 1] = w.y;
-              a[x][k + 2] = w.z;
-              a[x][k + 3] = w.w;
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            const uint32_t a0 = KvFormat<FMT>::template decode2<0>(a[0][k]);
-            const uint32_t a1 = KvFormat<FMT>::template decode2<0>(a[1][k]);
-            const uint32_t a2 = KvFormat<FMT>::template decode2<1>(a[0][k]);
-            const uint32_t a3 = KvFormat<FMT>::template decode2<1>(a[1][k]);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              mma_16816(s[mt][nt], a0, a1, a2, a3, qf[hf][k][nt][0], qf[hf][k][nt][1]);
-          }
-        }
-      }
-      // ---- masks, running maximum
-      const bool whole = t0 + kWarpTokens <= (p.causal ? at.len - at.n + 1 : at.len) &&
-                         (p.window <= 0 || t0 > at.len - 1 - p.window);
-      float most[NT][2];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float m = -INFINITY;
-#pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
+          for (int hf = 0; hf < HALVES; ++hf) {
+            uint32_t a[2][KS];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              float& z = s[mt][nt][2 * x + e];
-              z *= scales[mt] * qs[nt][e];
-              if (!whole) {
-                const int t = t0 + mt * 16 + x * 8 + g;
-                if (t > top[nt][e] || t < bottom[nt][e]) z = -INFINITY;
+  #pragma unroll
+              for (int k = 0; k < KS; k += 4) {
+                const uint4 w = lds128(kb + k_lane[k / 4] + hf * 128 + (mt * 16 + x * 8) * D);
+                a[x][k] = w.x;
+                a[x][k + 1] = w.y;
+                a[x][k + 2] = w.z;
+                a[x][k + 3] = w.w;
               }
-              m = fmaxf(m, z);
             }
-          most[nt][e] = m;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              const uint32_t a0 = KvFormat<FMT>::template decode2<0>(a[0][k]);
+              const uint32_t a1 = KvFormat<FMT>::template decode2<0>(a[1][k]);
+              const uint32_t a2 = KvFormat<FMT>::template decode2<1>(a[0][k]);
+              const uint32_t a3 = KvFormat<FMT>::template decode2<1>(a[1][k]);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                mma_16816(s[mt][nt], a0, a1, a2, a3, qf[hf][k][nt][0], qf[hf][k][nt][1]);
+            }
+          }
         }
-      bool grow = false;
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) grow |= most[nt][e] > mx[nt][e] + kLag;
-      const float v_top = fmaxf(v_ref, fmaxf(scales[2], scales[3]));
-      const bool v_grow = v_top > v_ref;
-      if (__any_sync(0xffffffffu, grow || v_grow)) {
-        const float vr = v_grow ? __fdividef(v_ref, v_top) : 1.0f;
-        v_ref = v_top;
+        // ---- masks, running maximum
+        const bool whole = t0 + kWarpTokens <= (p.causal ? at.len - at.n + 1 : at.len) &&
+                           (p.window <= 0 || t0 > at.len - 1 - p.window);
+        float most[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float m = most[nt][e];
+            float m = -INFINITY;
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-            m = fmaxf(m, mx[nt][e]);
-            const float f = m == -INFINITY ? 1.0f : fast_exp2(mx[nt][e] - m);
-            mx[nt][e] = m;
-            sum[nt][e] *= f;
+            for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-            for (int hf = 0; hf < HALVES; ++hf)
-#pragma unroll
-              for (int k = 0; k < KS; ++k) {
-                o[hf][k][nt][e] *= f * vr;
-                o[hf][k][nt][2 + e] *= f * vr;
+              for (int x = 0; x < 2; ++x) {
+                float& z = s[mt][nt][2 * x + e];
+                z *= scales[mt] * qs[nt][e];
+                if (!whole) {
+                  const int t = t0 + mt * 16 + x * 8 + g;
+                  if (t > top[nt][e] || t < bottom[nt][e]) z = -INFINITY;
+                }
+                m = fmaxf(m, z);
               }
+            most[nt][e] = m;
           }
-      }
-      // ---- p = 2^(s - m + 7), and o += p . v with dim as M, rows as N, tokens as K
-      const float inv_ref = __fdividef(1.0f, v_ref);
+        bool grow = false;
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
-        const float ratio = scales[2 + mt] * inv_ref;
-        uint32_t pb[NT][2];
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
+          for (int e = 0; e < 2; ++e) grow |= most[nt][e] > mx[nt][e] + kLag;
+        const float v_top = fmaxf(v_ref, fmaxf(scales[2], scales[3]));
+        const bool v_grow = v_top > v_ref;
+        if (__any_sync(0xffffffffu, grow || v_grow)) {
+          const float vr = v_grow ? __fdividef(v_ref, v_top) : 1.0f;
+          v_ref = v_top;
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float m = mx[nt][e] == -INFINITY ? 0.0f : mx[nt][e] - kShift;
+          for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              float& z = s[mt][nt][2 * x + e];
-              z = fast_exp2(z - m);
-              sum[nt][e] += z;
-              z *= ratio;
+            for (int e = 0; e < 2; ++e) {
+              float m = most[nt][e];
+#pragma unroll
+              for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+              m = fmaxf(m, mx[nt][e]);
+              const float f = m == -INFINITY ? 1.0f : fast_exp2(mx[nt][e] - m);
+              mx[nt][e] = m;
+              sum[nt][e] *= f;
+#pragma unroll
+              for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                  o[hf][k][nt][e] *= f * vr;
+                  o[hf][k][nt][2 + e] *= f * vr;
+                }
+            }
+        }
+        // ---- p = 2^(s - m + 7), and o += p . v with dim as M, rows as N, tokens as K
+        const float inv_ref = __fdividef(1.0f, v_ref);
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+          const float ratio = scales[2 + mt] * inv_ref;
+          uint32_t pb[NT][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float m = mx[nt][e] == -INFINITY ? 0.0f : mx[nt][e] - kShift;
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                float& z = s[mt][nt][2 * x + e];
+                z = fast_exp2(z - m);
+                sum[nt][e] += z;
+                z *= ratio;
+              }
+            }
+            pb[nt][0] = transpose_8x8(pack_half2(s[mt][nt][0], s[mt][nt][1]));
+            pb[nt][1] = transpose_8x8(pack_half2(s[mt][nt][2], s[mt][nt][3]));
+          }
+#pragma unroll
+          for (int hf = 0; hf < HALVES; ++hf) {
+            uint32_t w[4][KS / 2];                          // tokens 2c, 2c+1, 2c+8, 2c+9
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t at_x = vb + v_lane[x & 1] + hf * 128 + (mt * 16 + (x >> 1) * 8) * D;
+              if constexpr (D == 64) {
+                const uint2 y = lds64(at_x);
+                w[x][0] = y.x;
+                w[x][1] = y.y;
+              } else {
+                const uint4 y = lds128(at_x);
+                w[x][0] = y.x;
+                w[x][1] = y.y;
+                w[x][2] = y.z;
+                w[x][3] = y.w;
+              }
+            }
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+              const uint32_t sel = (k & 1) ? 0x7362u : 0x5140u;
+              const uint32_t lo = __byte_perm(w[0][k / 2], w[1][k / 2], sel);
+              const uint32_t hi = __byte_perm(w[2][k / 2], w[3][k / 2], sel);
+              const uint32_t a0 = KvFormat<FMT>::template decode2<0>(lo);
+              const uint32_t a1 = KvFormat<FMT>::template decode2<1>(lo);
+              const uint32_t a2 = KvFormat<FMT>::template decode2<0>(hi);
+              const uint32_t a3 = KvFormat<FMT>::template decode2<1>(hi);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                mma_16816(o[hf][k][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
             }
           }
-          pb[nt][0] = transpose_8x8(pack_half2(s[mt][nt][0], s[mt][nt][1]));
-          pb[nt][1] = transpose_8x8(pack_half2(s[mt][nt][2], s[mt][nt][3]));
-        }
-#pragma unroll
-        for (int hf = 0; hf < HALVES; ++hf) {
-          uint32_t w[4][KS / 2];                          // tokens 2c, 2c+1, 2c+8, 2c+9
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int r = mt * 16 + 2 * c + (x & 1) + (x >> 1) * 8;
-            if constexpr (D == 64) {
-              const uint2 y = lds64(vb + chunk_at<D>(r, g >> 1) + (g & 1) * 8);
-              w[x][0] = y.x;
-              w[x][1] = y.y;
-            } else {
-              const uint4 y = lds128(vb + chunk_at<D>(r, hf * 8 + g));
-              w[x][0] = y.x;
-              w[x][1] = y.y;
-              w[x][2] = y.z;
-              w[x][3] = y.w;
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            const uint32_t sel = (k & 1) ? 0x7362u : 0x5140u;
-            const uint32_t lo = __byte_perm(w[0][k / 2], w[1][k / 2], sel);
-            const uint32_t hi = __byte_perm(w[2][k / 2], w[3][k / 2], sel);
-            const uint32_t a0 = KvFormat<FMT>::template decode2<0>(lo);
-            const uint32_t a1 = KvFormat<FMT>::template decode2<1>(lo);
-            const uint32_t a2 = KvFormat<FMT>::template decode2<0>(hi);
-            const uint32_t a3 = KvFormat<FMT>::template decode2<1>(hi);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-              mma_16816(o[hf][k][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-          }
         }
       }
+      ends = at.tile + 1 == at.tile_end || i == units;
     }
-    if (++stage == kAttStages) stage = 0;
-    const bool ends = at.tile + 1 == at.tile_end;
-    if (!ends && u + 1 < units) {
-      ++at.tile;
-      continue;
-    }
-
-    // ---- the CTA's part of this (request, head, group) is done: its warps' results together,
-    // while the next one's queries are on their way
+    // The next one's queries are on their way while a (request, head, group) ends.
+    if ((i == 0 || ends) && i < units) load_queries(next);
     const Place done = at;
-    if (u + 1 < units) {
-      step(at);
-      load_queries(at);
-    }
+    at = next;
+    if (!ends) continue;
+
+    // ---- the CTA's part of this (request, head, group) is done: its warps' results together
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -628,7 +647,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             o[hf][k][nt][2 + e] *= f * v_ref;
           }
       }
-#pragma unroll
+#pragma unroll 1
     for (int live = WARPS; live > 1; live = (live + 1) / 2) {  // the upper half onto the lower
       const int half = (live + 1) / 2;
       if (warp >= half && warp < live) {
@@ -648,7 +667,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       }
       __syncthreads();
     }
-    const bool all_of_it = seg_tile == done.tile0 && ends;
+    const bool all_of_it = seg_tile == done.tile0 && done.tile + 1 == done.tile_end;
     // Output of rows by threads that hold values of dim 16 g + 2 k + {0, 1} (D = 64: 8 g + ...)
     const auto write = [&]() {
 #pragma unroll
@@ -685,11 +704,11 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       // Partial results: the part that begins at this CTA's first unit in its slot 0, one that
       // begins later (and so runs past its last) in slot 1.  A slot is its rows' maxima, their
       // sums, and the sums of weighted values [row][dim].
-      const int64_t first = u_begin + u - (done.tile - done.tile0);       // units of the whole
+      const int64_t first = u_begin + i - 1 - (done.tile - done.tile0);   // units of the whole
       const int64_t last = first + (done.tile_end - done.tile0) - 1;
-      const int32_t c0 = (int32_t)(((first + 1) * E - 1) / U), c1 = (int32_t)(((last + 1) * E - 1) / U);
+      const int32_t c0 = cta_of(first), c1 = cta_of(last);
       constexpr int PS = ROWS * (D + 2);
-      const int32_t odd = first > U * c0 / E ? 1 : 0;                 // the first part's slot
+      const int32_t odd = first > begins(c0) ? 1 : 0;                  // the first part's slot
       const auto slot_of = [&](int32_t k) {                           // of part k
         return p.partial + ((int64_t)(c0 + k) * 2 + (k == 0 ? odd : 0)) * PS;
       };
@@ -794,7 +813,8 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
     }
     fresh = true;
   }
-  if (bad) set_error(p.err, bad);
+  cp_async_wait_all();
+  if (p.apart) pdl_wait();
 }
 
 template <int D, int NT, int WARPS>
@@ -866,6 +886,7 @@ hs_status launch_kv_attend(AttendParams p, int32_t dim, int32_t format, int64_t 
     p.rows_most = kFewRows;
     if (const hs_status st = launch_kv_attend_tiles(p, dim, format, stream)) return st;
     if (!p.starts) return HS_OK;
+    p.apart = 1;
     rows = kFewRows;
   }
   return format == HS_KV_E4M3 ? launch_dim<HS_KV_E4M3>(p, dim, rows, stream)

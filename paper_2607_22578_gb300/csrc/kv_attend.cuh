@@ -33,6 +33,7 @@ struct AttendParams {
   int32_t causal;
   int32_t window;
   int32_t rows_most;         // requests with more rows (queries times G) are another kernel's
+  int32_t apart;             // the other kernel runs before this one on the stream
   float scale_log2;          // scale * log2(e)
   uint16_t* out;
   float* lse;
@@ -77,7 +78,7 @@ __device__ __forceinline__ int32_t attend_query(const AttendParams& p, int32_t r
 }
 
 // 8 values of 16 bits that are only 2-byte aligned
-__device__ __forceinline__ uint4 attend_raw8(const uint16_t* src) {
+static __device__ __noinline__ uint4 attend_raw8(const uint16_t* src) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
