@@ -68,6 +68,21 @@ struct Item {
   int32_t more;                      // 0: no further item
 };
 
+// The wait of kWaitLimitNs, out of line: the instruction cache is small beside this kernel.
+__device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort) {
+  const uint64_t t0 = globaltimer_ns();
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_try_wait(bar, parity)) return true;
+    if ((it & 63u) == 0) {
+      if (*abort) return false;
+      if (globaltimer_ns() - t0 > kWaitLimitNs) {
+        *abort = 1;
+        return false;
+      }
+    }
+  }
+}
+
 struct TilesShared {
   uint64_t item_full[kItemRing], item_empty[kItemRing];
   uint64_t q_full[2];
@@ -261,7 +276,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
   const uint32_t tmem = sh.tmem;
   volatile int* abort = &sh.abort;
   const auto wait = [&](uint64_t* bar, uint32_t phase) {  // a warp goes on, or gives up, as one
-    return __all_sync(0xffffffffu, mbar_wait(bar, phase & 1u, abort)) != 0;
+    const uint32_t a = smem_u32(bar);
+    return __all_sync(0xffffffffu, mbar_try_wait(a, phase & 1u) || wait_on(a, phase & 1u, abort)) != 0;
   };
 
   if (warp >= kLoadWarp && warp < kMmaWarp) {
@@ -583,24 +599,32 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       }
     };
     float qs = 0.0f;
-    const auto put = [&]() {
+    const auto put = [&]() {                        // a thread has a row, in place
       cp_async_wait_all();
-#pragma unroll 2
-      for (int i = 0; i < NQ; ++i) {
-        float f[8], big = 0.0f;
-        attend_unpack8(lds128(q_place(i)), p.fp16, f);
+      __syncwarp();
+      const uint32_t line = base + L::kQ + x * L::kTileBytes + row * 128;
+      uint32_t bits = 0;                            // the row's largest, as in 16 bits without a sign
+#pragma unroll 4
+      for (int ch = 0; ch < LR; ++ch) {
+        const uint4 v = lds128(line + (ch >> 3) * L::kBlockBytes + (((ch ^ row) & 7) << 4));
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) big = fmaxf(big, fabsf(f[e]));
-#pragma unroll
-        for (int o = 1; o < LR; o <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-        // a power of two of the row's size, kept where it and its inverse are normal
-        const uint32_t e = min(max(__float_as_uint(big) >> 23, 1u), 253u);
-        const float by = __uint_as_float((254u - e) << 23);
-        sts128(q_place(i), half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
-               half2_of(f[4] * by, f[5] * by), half2_of(f[6] * by, f[7] * by));
-        const uint32_t mine = __shfl_sync(0xffffffffu, e, (lane % RS) * LR);
-        if (lane / RS == i) qs = __uint_as_float(mine << 23) * p.scale_log2;
+        for (int e = 0; e < 4; ++e)
+          asm("max.u16x2 %0, %0, %1;" : "+r"(bits) : "r"(w[e] & 0x7fff7fffu));
       }
+      const float2 big = attend_unpack2(bits, p.fp16);
+      // a power of two of the row's size, kept where it and its inverse are normal
+      const uint32_t e = min(max(__float_as_uint(fmaxf(big.x, big.y)) >> 23, 1u), 253u);
+      const float by = __uint_as_float((254u - e) << 23);
+#pragma unroll 4
+      for (int ch = 0; ch < LR; ++ch) {
+        const uint32_t at = line + (ch >> 3) * L::kBlockBytes + (((ch ^ row) & 7) << 4);
+        float f[8];
+        attend_unpack8(lds128(at), p.fp16, f);
+        sts128(at, half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
+               half2_of(f[4] * by, f[5] * by), half2_of(f[6] * by, f[7] * by));
+      }
+      qs = __uint_as_float(e << 23) * p.scale_log2;
       fence_async_shared();
       mbar_arrive(&sh.q_full[x]);
     };
