@@ -68,6 +68,19 @@ struct Item {
   int32_t more;                      // 0: no further item
 };
 
+// Whether a phase is over, without waiting (try_wait may sleep until it is)
+__device__ __forceinline__ bool test_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+
 // The wait of kWaitLimitNs, out of line: the instruction cache is small beside this kernel.
 __device__ __noinline__ bool wait_on(uint32_t bar, uint32_t parity, volatile int* abort) {
   const uint64_t t0 = globaltimer_ns();
@@ -287,62 +300,64 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     constexpr int RG = (kTileTokens / 8 + kLoadWarps - 1) / kLoadWarps;  // groups of 8 tokens, mine
     constexpr int CH = D / 64;
 
-    // The tiles of this CTA's items end to end.  Of the one looked up (blocks only):
+    // The tiles of this CTA's items end to end: of the one whose blocks were looked up last, its
+    // item, and its blocks, place and length, for the loads to come.
     Item it{};
-    int32_t at = blockIdx.x, tile = 0;
-    uint32_t items = 0;                             // items said so far
-    bool ok = true, more = true;
-    const auto next_item = [&]() {                  // the next item, for everybody
-      it = Item{};
-      it.more = at < total;
-      if (it.more) {
-        int lo = 0, hi = kTilesThreads;             // the last thread with before <= at
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (sh.before[mid] <= at) lo = mid; else hi = mid;
+    int32_t at = blockIdx.x, tile = 0;              // the next item, and tile of `it`
+    uint32_t items = 0;                             // said so far
+    bool ok = true;
+    int32_t ids[RG], sid = -1, t_len = 0, t_h = 0, t_0 = 0;
+    const auto look_up = [&]() {                    // false: there is no further tile
+      if (tile == it.tile0 + it.tiles) {            // the next item, for everybody
+        it = Item{};
+        it.more = at < total;
+        if (it.more) {
+          int lo = 0, hi = kTilesThreads;           // the last thread with before <= at
+#pragma unroll 1
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (sh.before[mid] <= at) lo = mid; else hi = mid;
+          }
+          int32_t x = at - sh.before[lo], pairs = 0;
+          int32_t r = lo * per;
+#pragma unroll 1
+          for (;; ++r) {
+            pairs = request_pairs(p, r, it, &bad);
+            if (x < pairs * p.H || r + 1 >= min((lo + 1) * per, R)) break;
+            x -= pairs * p.H;
+          }
+          const int32_t back = x / p.H;
+          it.r = r;
+          it.h = x - back * p.H;
+          it.rows0 = max(pairs - 1 - back, 0) * kPairRows;
+          const int32_t before_q = it.len - it.n;   // the first query's position
+          if (p.window > 0)
+            it.tile0 = max(0, before_q + attend_query(p, it.rows0) - p.window + 1) / kTileTokens;
+          const auto steps = [&](int32_t first) {   // of the tile of rows that begins there
+            if (first >= it.rows) return 0;
+            const int32_t i1 = min(it.n - 1, attend_query(p, first + kTileRows - 1));
+            const int32_t see = p.causal ? min(it.len, before_q + i1 + 1) : it.len;
+            // (where nothing is seen: one, hidden)
+            return max(1, (see + kTileTokens - 1) / kTileTokens - it.tile0);
+          };
+          it.steps0 = steps(it.rows0);
+          it.steps1 = steps(it.rows0 + kTileRows);
+          it.tiles = max(it.steps0, it.steps1);
+          at += gridDim.x;
         }
-        int32_t x = at - sh.before[lo], pairs = 0;
-        int32_t r = lo * per;
-        for (;; ++r) {
-          pairs = request_pairs(p, r, it, &bad);
-          if (x < pairs * p.H || r + 1 >= min((lo + 1) * per, R)) break;
-          x -= pairs * p.H;
+        const uint32_t slot = items & (kItemRing - 1);
+        if (items >= kItemRing) ok = wait(&sh.item_empty[slot], items / kItemRing - 1);
+        if (lw == 0 && lane == 0 && ok) {
+          sh.items[slot] = it;
+          mbar_arrive(&sh.item_full[slot]);
         }
-        it.r = r;
-        it.h = x % p.H;
-        it.rows0 = max(pairs - 1 - x / p.H, 0) * kPairRows;
-        const int32_t before_q = it.len - it.n;     // the first query's position
-        if (p.window > 0)
-          it.tile0 = max(0, before_q + attend_query(p, it.rows0) - p.window + 1) / kTileTokens;
-        const auto steps = [&](int32_t first) {     // of the tile of rows that begins there
-          if (first >= it.rows) return 0;
-          const int32_t i1 = min(it.n - 1, attend_query(p, first + kTileRows - 1));
-          const int32_t see = p.causal ? min(it.len, before_q + i1 + 1) : it.len;
-          // (where nothing is seen: one, hidden)
-          return max(1, (see + kTileTokens - 1) / kTileTokens - it.tile0);
-        };
-        it.steps0 = steps(it.rows0);
-        it.steps1 = steps(it.rows0 + kTileRows);
-        it.tiles = max(it.steps0, it.steps1);
-        at += gridDim.x;
+        ++items;
+        tile = it.tile0;
+        if (!ok || !it.more) return false;
       }
-      const uint32_t slot = items & (kItemRing - 1);
-      if (items >= kItemRing) ok = ok && wait(&sh.item_empty[slot], items / kItemRing - 1);
-      if (lw == 0 && lane == 0 && ok) {
-        sh.items[slot] = it;
-        mbar_arrive(&sh.item_full[slot]);
-      }
-      ++items;
-      more = it.more;
-      tile = it.tile0;
-    };
-
-    int32_t ids[RG], t_len = 0, t_h = 0, t_0 = 0;   // of the tile that is fetched next
-    int32_t sid = -1;
-    const auto look_up = [&]() {                    // its blocks, and one tile on
       t_len = it.len;
       t_h = it.h;
-      t_0 = tile * kTileTokens;
+      t_0 = tile++ * kTileTokens;
       const int32_t* row = p.table + (int64_t)it.r * p.width;
 #pragma unroll
       for (int i = 0; i < RG; ++i) {
@@ -351,23 +366,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       }
       if (lw == 0 && lane < kGroups)
         sid = t_0 + lane * 16 < t_len ? __ldg(row + ((t_0 + lane * 16) >> p.bt_log2)) : -1;
-      if (++tile == it.tile0 + it.tiles) next_item();
+      return true;
     };
-    int64_t off[RG];                                // of this thread's 16 bytes; -1: no token
     uint4 kr[RG][CH], vr[RG][CH];
-    float4 sc = make_float4(0.f, 0.f, 0.f, 0.f);
-    const auto place = [&]() {
-#pragma unroll
-      for (int i = 0; i < RG; ++i) {
-        const int32_t tok = t_0 + (lw + i * kLoadWarps) * 8 + row8, id = ids[i];
-        const bool known = (uint32_t)id < (uint32_t)p.n_blocks;
-        if (id != -1 && !known) bad = kErrInvalidArg;
-        off[i] = known && tok < t_len
-                     ? ((((int64_t)id * p.H + t_h) << p.bt_log2) + (tok & ((1 << p.bt_log2) - 1))) * D +
-                           chunk * 16
-                     : -1;
-      }
-    };
+    int64_t off[RG];                                // of this thread's 16 bytes; -1: no token
+    float2 scale = make_float2(0.0f, 0.0f);         // of 16 tokens, for this lane
     const auto fetch = [&](const uint8_t* codes, uint4 (&to)[RG][CH]) {
 #pragma unroll
       for (int i = 0; i < RG; ++i)
@@ -375,15 +378,6 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         for (int c = 0; c < CH; ++c)
           to[i][c] = off[i] >= 0 ? __ldg(reinterpret_cast<const uint4*>(codes + off[i] + c * 64))
                                  : make_uint4(0u, 0u, 0u, 0u);
-    };
-    const auto fetch_scale = [&]() {
-      if (lw == 0 && lane < kGroups) {
-        const bool in = (uint32_t)sid < (uint32_t)p.n_blocks;
-        if (!in && t_0 + lane * 16 < t_len) bad = kErrInvalidArg;
-        const float a = in ? __ldg(p.ks + (int64_t)sid * p.H + t_h) : 0.0f;
-        const float b = in ? __ldg(p.vs + (int64_t)sid * p.H + t_h) : 0.0f;
-        sc = make_float4(a, b, 0.f, 0.f);
-      }
     };
     const auto put = [&](uint32_t to, const uint4 (&from)[RG][CH]) {
 #pragma unroll
@@ -406,41 +400,51 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         }
       }
     };
-    next_item();
-    bool fetched = more && ok;
-    if (fetched) {
-      look_up();
-      place();
-      fetch(p.k, kr);
-      fetch(p.v, vr);
-      fetch_scale();
-    }
-    bool looked = more && ok;
-    if (fetched && looked) look_up();
-    for (uint32_t n = 0; fetched && ok; ++n) {
-      const uint32_t st = n & 1, use = n >> 1;
-      if (n >= 2 && !(ok = wait(&sh.k_empty[st], use - 1))) break;
-      if (lw == 0 && lane < kGroups) {
-        const float v = sc.y < kLeastScale ? kLeastScale : sc.y;  // (a NaN stays one)
-        sh.scales[n & (kScaleRing - 1)][lane] =
-            make_float4(sc.x < kLeastScale ? kLeastScale : sc.x, log2f(v), __fdividef(1.0f, v), 0.f);
+    // Round n lays out tile n - 1 and fetches tile n into the registers that get free.
+    bool looked = look_up(), fetched = false;
+#pragma unroll 1
+    for (uint32_t n = 0; ok && (looked || fetched); ++n) {
+      const uint32_t st = (n - 1) & 1, use = (n - 1) >> 1;
+      if (fetched) {
+        if (n > 2 && !(ok = wait(&sh.k_empty[st], use - 1))) break;
+        if (lw == 0 && lane < kGroups) {
+          const float k = scale.x < kLeastScale ? kLeastScale : scale.x;  // (a NaN stays one)
+          const float v = scale.y < kLeastScale ? kLeastScale : scale.y;
+          sh.scales[(n - 1) & (kScaleRing - 1)][lane] =
+              make_float4(k, log2f(v), __fdividef(1.0f, v), 0.0f);
+        }
+        put(base + L::kK + st * L::kTileBytes, kr);
+        fence_async_shared();
+        mbar_arrive(&sh.k_full[st]);
       }
-      put(base + L::kK + st * L::kTileBytes, kr);
-      fence_async_shared();
-      mbar_arrive(&sh.k_full[st]);
       if (looked) {
-        place();
+#pragma unroll
+        for (int i = 0; i < RG; ++i) {
+          const int32_t tok = t_0 + (lw + i * kLoadWarps) * 8 + row8, id = ids[i];
+          const bool known = (uint32_t)id < (uint32_t)p.n_blocks;
+          if (id != -1 && !known) bad = kErrInvalidArg;
+          off[i] = known && tok < t_len
+                       ? ((((int64_t)id * p.H + t_h) << p.bt_log2) +
+                          (tok & ((1 << p.bt_log2) - 1))) * D + chunk * 16
+                       : -1;
+        }
         fetch(p.k, kr);
-        fetch_scale();
+        if (lw == 0 && lane < kGroups) {
+          const bool in = (uint32_t)sid < (uint32_t)p.n_blocks;
+          if (!in && t_0 + lane * 16 < t_len) bad = kErrInvalidArg;
+          scale.x = in ? __ldg(p.ks + (int64_t)sid * p.H + t_h) : 0.0f;
+          scale.y = in ? __ldg(p.vs + (int64_t)sid * p.H + t_h) : 0.0f;
+        }
       }
-      if (n >= 2 && !(ok = wait(&sh.v_empty[st], use - 1))) break;
-      put(base + L::kV + st * L::kTileBytes, vr);
-      fence_async_shared();
-      mbar_arrive(&sh.v_full[st]);
+      if (fetched) {
+        if (n > 2 && !(ok = wait(&sh.v_empty[st], use - 1))) break;
+        put(base + L::kV + st * L::kTileBytes, vr);
+        fence_async_shared();
+        mbar_arrive(&sh.v_full[st]);
+      }
       if (looked) fetch(p.v, vr);
       fetched = looked;
-      looked = more && looked;
-      if (looked) look_up();
+      if (looked) looked = look_up();
     }
   } else if (warp == kMmaWarp) {
     // ================================ products
@@ -563,7 +567,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         if (block) {
           if (!(ok = wait(&sh.item_full[slot], phase))) return false;
         } else if (!__all_sync(0xffffffffu,
-                               mbar_try_wait(smem_u32(&sh.item_full[slot]), phase & 1u))) {
+                               test_wait(smem_u32(&sh.item_full[slot]), phase & 1u))) {
           return false;
         }
         next = sh.items[slot];
@@ -582,19 +586,25 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       return q_line + r * 128 + (((q_chunk ^ r) & 7) << 4);
     };
     const auto fetch = [&]() {
-      const int32_t first = next.rows0 + x * kTileRows + q_row;
-      const uint16_t* heads = p.q + (int64_t)next.h * p.G * p.q_head + q_chunk * 8;
-#pragma unroll 4
+      const int32_t first = min(next.rows0 + x * kTileRows + q_row, next.rows - 1);
+      const int32_t left = next.rows - (next.rows0 + x * kTileRows + q_row);
+      const int32_t a = attend_query(p, first);
+      int32_t b = first - a * p.G;                  // its head of the group
+      const uint16_t* src = p.q + (int64_t)(next.q0 + a) * p.q_token +
+                            (int64_t)(next.h * p.G + b) * p.q_head + q_chunk * 8;
+      const int64_t wrap = p.q_token - (int64_t)p.G * p.q_head;  // on to the next query
+#pragma unroll 2
       for (int i = 0; i < NQ; ++i) {
-        const int32_t full = first + i * RS;
-        const bool in = full < next.rows;
-        const int32_t a = in ? attend_query(p, full) : 0, b = in ? full - a * p.G : 0;
-        const uint16_t* src = heads + (int64_t)(next.q0 + a) * p.q_token + (int64_t)b * p.q_head;
+        const bool in = i * RS < left;
         if (p.q_vec) {
           cp_async16_zfill(q_place(i), src, in);
         } else {
           const uint4 v = in ? attend_raw8(src) : make_uint4(0u, 0u, 0u, 0u);
           sts128(q_place(i), v.x, v.y, v.z, v.w);
+        }
+        if ((i + 1) * RS < left) {                  // to the row after the load's
+          src += RS * p.q_head;
+          for (b += RS; b >= p.G; b -= p.G) src += wrap;
         }
       }
     };
@@ -724,10 +734,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
           }
           tmem_ld_wait();
           if (t0 < from || t0 + kHalfTokens - 1 > to) {
-            const int32_t last = top - t0, first = bottom - t0;
+            // a bit for each token that is seen
+            const int32_t last = min(max(top - t0, -1), kHalfTokens - 1);
+            const int32_t first = max(bottom - t0, 0);
+            const uint64_t seen = last < first ? 0ull : (~0ull >> (63 - last)) & (~0ull << first);
+            const uint32_t lo = (uint32_t)seen, hi = (uint32_t)(seen >> 32);
 #pragma unroll
             for (int e = 0; e < kHalfTokens; ++e)
-              if (e > last || e < first) a[e] = 0xff800000u;  // -inf
+              if (!((e < 32 ? lo : hi) & (1u << (e & 31)))) a[e] = 0xff800000u;  // -inf
           }
           // ---- the maximum of acc * c + lv
           float b[kHalfGroups];
