@@ -15,7 +15,7 @@ from ._lib import (HS_ERR_CUDA, HS_ERR_INVALID_ARG, HS_ERR_TIMEOUT, HS_ERR_UNSUP
                    hs_cache_lookup, hs_cache_stats,
                    hs_unique_inverse, hs_unique_inverse_noalloc, hs_unique_inverse_workspace,
                    hs_version, library_path, load)
-from .pipeline import EmbedRetrieveStage, HostFeed, RetrieveGraph, StepGraph
+from .pipeline import EmbedRetrieveStage, HostFeed, KvRequests, RetrieveGraph, StepGraph
 
 __all__ = [
     "HS_OK", "HS_ERR_INVALID_ARG", "HS_ERR_UNSUPPORTED", "HS_ERR_CUDA", "HS_ERR_WORKSPACE",
@@ -30,5 +30,5 @@ __all__ = [
     "hs_debug_scan_wait", "hs_debug_stream_rows", "hs_debug_merge_key_mask",
     "hs_debug_retrieve_wait", "hs_merge_rows",
     "hs_merge_rows_workspace", "hs_version",
-    "library_path", "load", "EmbedRetrieveStage", "HostFeed", "RetrieveGraph", "StepGraph",
+    "library_path", "load", "EmbedRetrieveStage", "HostFeed", "KvRequests", "RetrieveGraph", "StepGraph",
 ]

@@ -16,6 +16,10 @@ Composition of the C-ABI calls only (no arithmetic here):
   rerank:  hs_retrieve_topk_n -> hs_scatter_results (rerank vectors of the
            merged queries) -> hs_rerank_topk        (top-k rescored, best kept,
                                                      fanned out; Section 4.1)
+  requests: hs_merge_rows of the prompts -> hs_scatter_results (lengths of the
+           merged ones) -> hs_kv_tables; then a layer at a time hs_kv_append ->
+           hs_kv_attend, and hs_kv_release at the end (KvRequests: the merged
+           model calls of a batch, each run once over one cache)
 Nothing here synchronises with the host: the merged-query count stays in
 device memory (the retrieval reads it when its kernels run), and the
 unique-index tail beyond that count is a valid row map, so the gather can
@@ -352,3 +356,82 @@ class HostFeed:
         """Wait for a submitted batch; returns host (scores, ids, n_unique)."""
         self.done[slot].synchronize()
         return self.h_s[slot], self.h_i[slot], int(self.h_nu[slot][0])
+
+
+class KvRequests:
+    """The model calls of a batch of workflows, merged, as requests over one
+    paged cache: which blocks each has, how far each has come, and which
+    blocks are free.
+
+    ``begin`` merges equal prompts and gives each merged one its blocks,
+    ``extend`` the same to the tokens of a later step; both say where the
+    step's tokens go (slots) and which request each belongs to (starts).  Then,
+    for every layer's cache of the same shape, ``append`` writes the step's
+    keys and values and ``attend`` runs its queries; ``release`` gives a
+    finished request's blocks back.  The number of merged requests stays in
+    device memory (``n_req``), as everywhere here."""
+
+    def __init__(self, cache: "_lib.KvCache", max_requests: int, max_len: int):
+        dev = cache.k.device
+        i32 = dict(dtype=torch.int32, device=dev)
+        self.block_tokens, self.n_blocks = cache.block_tokens, cache.n_blocks
+        self.max_requests = int(max_requests)
+        width = -(-int(max_len) // cache.block_tokens)
+        self.table = torch.full((self.max_requests, width), -1, **i32)
+        self.lens = torch.zeros(self.max_requests, **i32)
+        self.n_req = torch.zeros(1, **i32)
+        self.pool = torch.arange(cache.n_blocks, **i32)
+        self.cursor = torch.tensor([0, cache.n_blocks], dtype=torch.int64, device=dev)
+        self.slots = self.starts = None
+        self.max_q = 0
+        self._ws = {}
+
+    def begin(self, tokens: torch.Tensor, lens: torch.Tensor | None = None):
+        """New requests for the prompts tokens [n, stride] (int32, ``lens`` of
+        them valid): equal ones are one request.  Returns (slots, starts,
+        unique_idx, inverse): request u's tokens are those of prompt
+        unique_idx[u], prompt i is request inverse[i]."""
+        n, stride = tokens.shape
+        if n > self.max_requests:
+            raise ValueError("more prompts than max_requests")
+        if lens is None:
+            lens = torch.full((n,), stride, dtype=torch.int32, device=tokens.device)
+        _, self.n_req, unique_idx, inverse = _lib.hs_merge_rows(tokens, lens)
+        fresh = torch.zeros(self.max_requests, dtype=torch.int32, device=tokens.device)
+        _lib.hs_scatter_results(lens, unique_idx, dst=fresh[:n])
+        self.lens.zero_()
+        return self.extend(fresh, n * stride, stride) + (unique_idx, inverse)
+
+    def extend(self, fresh: torch.Tensor, max_tokens: int, max_q: int):
+        """Blocks and slots for fresh[r] more tokens of each request (at most
+        max_q each and max_tokens in all).  Returns (slots, starts)."""
+        self.slots, self.starts, self.lens, self.cursor = _lib.hs_kv_tables(
+            self.lens, fresh, self.table, self.pool, self.cursor, self.block_tokens, max_tokens,
+            n_req_dev=self.n_req)
+        self.max_q = int(max_q)
+        return self.slots, self.starts
+
+    def append(self, cache: "_lib.KvCache", k: torch.Tensor, v: torch.Tensor) -> None:
+        """The step's keys and values [max_tokens, n_kv_heads, dim]."""
+        _lib.hs_kv_append(cache, k, v, self.slots)
+
+    def attend(self, cache: "_lib.KvCache", q: torch.Tensor, scale: float | None = None,
+               window: int = 0):
+        """The step's queries [max_tokens, n_heads, dim] over all that their
+        request has.  Returns (out, lse); rows past the step's tokens are not
+        written."""
+        key = (q.shape[1], cache.dim)
+        if key not in self._ws:
+            self._ws[key] = torch.zeros(
+                _lib.hs_kv_attend_workspace(cache, q.shape[1], self.max_q), dtype=torch.uint8,
+                device=q.device)
+        return _lib.hs_kv_attend(cache, q, self.lens, self.table, starts=self.starts,
+                                 max_q=self.max_q, scale=scale, window=window,
+                                 n_req_dev=self.n_req, workspace=self._ws[key])
+
+    def release(self, done: torch.Tensor) -> None:
+        """Give back the blocks of the requests with done[r] (bool
+        [max_requests]); they have no tokens after that."""
+        self.cursor = _lib.hs_kv_release(torch.where(done, self.lens, 0), self.table, self.pool,
+                                         self.cursor, self.block_tokens, n_req_dev=self.n_req)
+        self.lens = torch.where(done, 0, self.lens)
