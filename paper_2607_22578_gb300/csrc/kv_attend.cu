@@ -879,6 +879,7 @@ hs_status launch_kv_attend(AttendParams p, int32_t dim, int32_t format, int64_t 
   p.err = device_error_word();
   if (!p.err) return fail(HS_ERR_CUDA, "could not resolve the device error word");
   p.counters = static_cast<unsigned*>(ws);
+  p.queue = p.counters + attend_counters();
   p.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + attend_counter_bytes());
   p.rows_most = 0x7fffffff;
   if (dim <= 128 && rows > kFewRows) {
