@@ -727,9 +727,14 @@ hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, i
  * lse         float [n_tokens, n_heads], or NULL.
  * workspace   hs_kv_attend_workspace() bytes, 256-byte aligned, zeroed once
  *             before its first use; every call leaves it fit for the next.
- * Products of 16-bit values with fp32 sums; q, k and v are exact in them, the
- * weights are rounded to half.  Results do not depend on the order in which
- * the kernel's blocks finish.
+ * Products of 16-bit values with fp32 sums; k and v are exact in them, q but
+ * for what is below 2^-24 of its row's largest value, the weights are rounded
+ * to half.  Results do not depend on the order in which the kernel's blocks
+ * finish.
+ * Slots past a request's end are never read as numbers, whatever they hold.  A
+ * NaN or an infinite scale among a request's own tokens is seen by every query
+ * that sees the token, and a NaN value of v (its column) also by the queries
+ * of the same call and request that stand before it.
  * Device errors (HS_ERR_INVALID_ARG in the error word): starts or lens that
  * cannot be (the request's rows are left as they were), a table entry that is
  * no block (its tokens count as zeros).

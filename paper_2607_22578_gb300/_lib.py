@@ -793,9 +793,12 @@ def hs_kv_attend(cache: KvCache, q: torch.Tensor, lens: torch.Tensor, table: tor
         if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2]
                                 or not lse.is_cuda or not lse.is_contiguous()):
             raise ValueError("lse must be contiguous float32 [tokens, n_heads]")
-    if workspace is None:
-        workspace = torch.zeros(hs_kv_attend_workspace(cache, heads, max_q), dtype=torch.uint8,
-                                device=q.device)
+    if workspace is None:                       # zeroed on the stream that uses it
+        on = stream if stream is None or isinstance(stream, torch.cuda.Stream) else \
+            torch.cuda.ExternalStream(int(stream), device=q.device)
+        with torch.cuda.stream(on):
+            workspace = torch.zeros(hs_kv_attend_workspace(cache, heads, max_q),
+                                    dtype=torch.uint8, device=q.device)
     _check((_lib or load()).hs_kv_attend(
         cache._at, q.data_ptr(), dtype, T, heads, by[0], by[1], lens.data_ptr(), sp, n,
         None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"), max_q, table.data_ptr(),

@@ -213,11 +213,12 @@ def test_the_same_twice_on_one_workspace():
     """Cut requests are merged in the order of their parts, and the workspace is left as found."""
     a = problem([40003, 900], [1, 1], 2, 4, 128, 16, "e4m3", "bf16")
     b = problem([3000] * 7, [3] * 7, 2, 6, 64, 32, "int8", "fp16")
-    size = max(hs.hs_kv_attend_workspace(p["cache"], 12, 3) for p in (a, b))
+    c = problem([700, 90, 2000, 1], [300, 90, 70, 1], 2, 4, 128, 16, "e4m3", "bf16")
+    size = max(hs.hs_kv_attend_workspace(p["cache"], 12, 300) for p in (a, b, c))
     ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
-    want = [call(p) for p in (a, b)]
+    want = [call(p) for p in (a, b, c)]
     for _ in range(5):
-        for p, w in zip((a, b), want):
+        for p, w in zip((a, b, c), want):
             got = call(p, workspace=ws)
             assert torch.equal(got[0], w[0]) and torch.equal(got[1], w[1])
 
@@ -231,6 +232,9 @@ def test_on_another_stream_and_in_a_graph():
     s.wait_stream(torch.cuda.current_stream())
     got = hs.hs_kv_attend(p["cache"], p["q"], lens, p["table"], starts=starts, max_q=1,
                           workspace=ws, stream=s)
+    s.synchronize()
+    assert torch.equal(got[0], want[0])
+    got = hs.hs_kv_attend(p["cache"], p["q"], lens, p["table"], starts=starts, max_q=1, stream=s)
     s.synchronize()
     assert torch.equal(got[0], want[0])
     g = torch.cuda.CUDAGraph()
@@ -258,6 +262,19 @@ def test_offsets_past_32_bits(n):
     want = call(p)
     got = call(dict(p, cache=far, table=to.int()[None]))
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_no_queries_and_no_requests():
+    p = problem([30, 7], [1, 1], 2, 4, 64, 16, "e4m3", "bf16")
+    none = p["q"][:0]
+    for lens, table in ((dev(p["lens"]), p["table"]), (dev([]), p["table"][:0])):
+        out, lse = hs.hs_kv_attend(p["cache"], none, lens, table)
+        assert out.shape == none.shape and lse.shape == (0, 8)
+    out = (torch.full_like(p["q"], 5.0), torch.full((2, 8), 5.0, device="cuda"))
+    hs.hs_kv_attend(p["cache"], p["q"], dev(p["lens"]), p["table"], starts=dev([0, 0, 2]), max_q=2,
+                    out=out)
+    hs.hs_get_device_error()                           # the first request has none
+    assert (out[0] != 5).all()
 
 
 def expect_error():
