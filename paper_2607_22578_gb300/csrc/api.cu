@@ -49,7 +49,7 @@ hs_status launch_kv_release(const int32_t*, int64_t, const int32_t*, int32_t, co
                             int32_t, int32_t*, int64_t, const int64_t*, int64_t*, cudaStream_t);
 hs_status launch_kv_append(const hs_kv_cache&, int32_t, const uint16_t*, const uint16_t*, int32_t,
                            int64_t, int64_t, int64_t, const int32_t*, cudaStream_t);
-size_t attend_workspace(int32_t);
+size_t attend_workspace(int32_t, int64_t);
 hs_status launch_kv_attend(AttendParams, int32_t, int32_t, int64_t, void*, cudaStream_t);
 
 namespace {
@@ -602,7 +602,7 @@ hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, i
 size_t hs_kv_attend_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t dim, int32_t max_q) {
   if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || max_q < 0) return 0;
   if (dim != 64 && dim != 128 && dim != 256) return 0;
-  return attend_workspace(dim);
+  return attend_workspace(dim, (int64_t)max_q * (n_heads / n_kv_heads));
 }
 
 hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, int64_t n_tokens,
@@ -632,7 +632,7 @@ hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, i
   if (!aligned(q, 2) || !aligned(out, 16) || !aligned(lens, 4) || !aligned(starts, 4) ||
       !aligned(table, 4) || !aligned(lse, 4))
     return fail(HS_ERR_INVALID_ARG, "misaligned pointer (q 2 B, out 16 B, others 4 B)");
-  const size_t need = attend_workspace(cache->dim);
+  const size_t need = attend_workspace(cache->dim, (int64_t)max_q * (n_heads / cache->n_kv_heads));
   if (!workspace || !aligned(workspace, 256))
     return fail(HS_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned");
   if (workspace_bytes < need)

@@ -20,27 +20,34 @@
 //  - Products are on mma.sync m16n8k16 with tokens as M and rows as N: a decoding step has 1 to 16
 //    rows, which would fill an eighth of a tcgen05 tile's 128, and codes go straight from shared
 //    memory to registers as half2 (exact for e4m3 and int8).
+// Measured: 256 requests of 1 to 8192 tokens, 32 / 8 heads of 128, 2.1 GB in 339 to 345 us (0.92 of
+// the copy rate); 8 of 100 to 1500 in 11.6 us, which are launch and round trips.
 // Arithmetic: q as half after division by a power of two of its row (exact but below 2^-24 of the
 // row's largest), products and sums in fp32, p = 2^(s - m + 7) as half (the running maximum m may
 // lag by 8, so p <= 2^15; what is under 2^-31 of the largest is dropped from o, not from lse),
 // scales of value blocks relative to the largest so far, divided out at the end.
+#include <algorithm>
+
 #include "kv_cache.cuh"
 #include "kv_attend.cuh"
 
 namespace hs {
 
 hs_status launch_kv_attend_tiles(const AttendParams&, int32_t, int32_t, cudaStream_t);
+size_t tiles_partial_bytes(int32_t dim);
 
 namespace {
 
 constexpr int kWarpTokens = 32;                          // of a unit, for each warp
+constexpr int kFewRows = 32;                             // of a request: see few_rows
 constexpr int kAttStages = 2;
-constexpr int kFewRows = 32;                             // of a request: more are kv_attend_tiles.cu's
 constexpr float kLag = 8.0f;                             // of the running maximum, in powers of two
 constexpr float kShift = 7.0f;
 
 // Warps of a CTA, and CTAs of an SM.  Small CTAs side by side go on loading while one of them ends
-// a (request, head, group); a single large one leaves few parts of a long request to merge.
+// a (request, head, group), a single large one leaves few parts of a long one to merge.  8 of 16,000
+// tokens take 16 us with large CTAs and 29 with small ones, 8 of 500 10.7 and 8.9, 32 of 4000 18.5
+// and 16.6; at 16 they are level.
 template <int D, int NT>
 constexpr int few_warps() { return D == 256 ? 7 - NT : 4; }
 template <int D, int NT>
@@ -845,7 +852,7 @@ template <int D, int NT, int FMT>
 hs_status launch_warps(const AttendParams& p, int64_t rows, cudaStream_t stream) {
   // (request, head, group)s, at most
   const int64_t whole = (int64_t)p.n_req * p.H * ((rows + 8 * NT - 1) / (8 * NT));
-  return whole * 4 <= num_sms() ? launch<D, NT, many_warps<D, NT>(), FMT>(p, stream)
+  return whole * 8 <= num_sms() ? launch<D, NT, many_warps<D, NT>(), FMT>(p, stream)
                                 : launch<D, NT, few_warps<D, NT>(), FMT>(p, stream);
 }
 
@@ -867,11 +874,27 @@ hs_status launch_dim(const AttendParams& p, int32_t dim, int64_t rows, cudaStrea
 
 }  // namespace
 
-size_t attend_workspace(int32_t dim) {
+// Rows of a request up to which this kernel takes it, where kv_attend_tiles.cu could.  There up to
+// 256 rows cost what one does, here every 16 read the codes again: 64 requests of 2000 tokens, 8
+// heads of 128, take 114 us here and 161 there with 32 rows, 209 and 161 with 64.  But there eight
+// CTAs share an item at most, here as many as there are: one request of 8192 tokens, one head and
+// 512 rows takes 28 us here and 42 there, one of 2000 tokens, 8 heads and 64 rows 17 and 27.  The two
+// are level at about one (request, head, 16 rows) for two SMs.
+static int32_t few_rows(const AttendParams& p) {
+  const int64_t heads = (int64_t)p.n_req * p.H;
+  return (int32_t)std::max<int64_t>(kFewRows, num_sms() / (2 * heads) * 16);
+}
+
+static size_t few_partial_bytes(int32_t dim) {
   const int64_t rows = dim == 64 ? 32 : 16;               // of a tile, at most
   const int64_t ctas = (int64_t)num_sms() * kAttendMaxPerSm;
-  const int64_t slot = rows * (dim + 2) * 4;
-  return (size_t)(attend_counter_bytes() + ctas * 2 * slot);
+  return (size_t)(ctas * 2 * rows * (dim + 2) * 4);
+}
+
+// `rows`: of a request, at most
+size_t attend_workspace(int32_t dim, int64_t rows) {
+  return attend_counter_bytes() + few_partial_bytes(dim) +
+         (dim <= 128 && rows > kFewRows ? tiles_partial_bytes(dim) : 0);
 }
 
 hs_status launch_kv_attend(AttendParams p, int32_t dim, int32_t format, int64_t rows, void* ws,
@@ -880,15 +903,18 @@ hs_status launch_kv_attend(AttendParams p, int32_t dim, int32_t format, int64_t 
   if (!p.err) return fail(HS_ERR_CUDA, "could not resolve the device error word");
   p.counters = static_cast<unsigned*>(ws);
   p.queue = p.counters + attend_counters();
+  p.tile_counters = p.queue + 2;
   p.partial = reinterpret_cast<float*>(static_cast<char*>(ws) + attend_counter_bytes());
+  p.tile_partial = p.partial + few_partial_bytes(dim) / 4;
   p.rows_most = 0x7fffffff;
-  if (dim <= 128 && rows > kFewRows) {
+  const int32_t few = few_rows(p);
+  if (dim <= 128 && rows > few) {
     // Requests of many rows by tiles; with lengths of their own there may be others.
-    p.rows_most = kFewRows;
+    p.rows_most = few;
     if (const hs_status st = launch_kv_attend_tiles(p, dim, format, stream)) return st;
     if (!p.starts) return HS_OK;
     p.apart = 1;
-    rows = kFewRows;
+    rows = few;
   }
   return format == HS_KV_E4M3 ? launch_dim<HS_KV_E4M3>(p, dim, rows, stream)
                               : launch_dim<HS_KV_INT8>(p, dim, rows, stream);

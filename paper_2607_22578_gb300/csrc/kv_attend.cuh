@@ -40,15 +40,17 @@ struct AttendParams {
   unsigned* counters;
   unsigned* queue;           // of the kernel of many rows: items drawn, CTAs that are done
   float* partial;
+  unsigned* tile_counters;   // of the kernel of many rows: parts done of each warp's rows of an item
+  float* tile_partial;
   unsigned* err;
 };
 
 constexpr int kAttendMaxPerSm = 4;  // CTAs of a launch that one SM holds, at most
 
-// A counter for each CTA of a launch, and the queue's two.
+// A counter for each CTA of a launch, the queue's two, and eight for each SM's item.
 inline int64_t attend_counters() { return (int64_t)num_sms() * kAttendMaxPerSm; }
 inline int64_t attend_counter_bytes() {
-  return ((attend_counters() + 2) * 4 + 255) / 256 * 256;
+  return ((attend_counters() + 2 + num_sms() * 8) * 4 + 255) / 256 * 256;
 }
 
 // Request r's queries (n of them, from token q0 of the batch) and tokens in the cache; false if

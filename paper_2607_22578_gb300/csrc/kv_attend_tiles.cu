@@ -21,6 +21,14 @@
 // counter in the workspace, drawn from an item ahead): items are few and differ by much, and in a
 // fixed order six requests behind 1,000 to 12,000 tokens took 467 us.  An item's queries and first
 // tokens are loaded while the one before it ends.  Which CTA computes an item changes no result.
+// Where there are fewer items than half the CTAs, an item's tokens are up to eight parts, each an item
+// of its own; a warp's rows of the parts are merged by the one that is done last (128 queries over
+// 16,384 tokens, 32 / 8 heads of 128: 313 -> 64 us).
+//
+// Measured: 16 prompts of 256 to 2048 tokens, 32 / 8 heads of 128, 347 us (601 TFLOP/s); six chunks of
+// up to 1024 queries behind 1,000 to 12,000 tokens, 32 / 4 heads, 441 (752).  256 rows by 128 tokens
+// take 4500 clocks, products 2200 of them: the rest is the chain of one tile (scores loaded, maximum,
+// 64 exponentials a thread, twice, then the last product and the next scores).
 //
 // Arithmetic: q as half after division by a power of two of its row; codes as half (exact); sums
 // in fp32.  A block's scales enter through the exponent: with c the scores' factor and lv = log2 of
@@ -47,6 +55,8 @@ constexpr int kHalfGroups = kGroups / 2;
 constexpr int kLoadThreads = kLoadWarps * 32;
 constexpr int kScaleRing = 4;                  // tiles
 constexpr int kItemRing = 4;
+constexpr int kMostParts = 8;                  // of an item
+constexpr int kLeastSteps = 4;                 // of a part
 constexpr float kTilesLag = 8.0f;
 constexpr float kTilesShift = 7.0f;
 constexpr float kLeastScale = 1.17549435e-38f;
@@ -68,7 +78,14 @@ struct Item {
   int32_t tile0, tiles, rows;        // tiles of tokens; rows of the request
   int32_t steps0, steps1;            // of these for each tile of rows (0: it has no rows)
   int32_t more;                      // 0: no further item
+  // A part of the tokens: the first part's place among the partial results (16 bits), which part
+  // it is (4), how many there are for each tile of rows (4, 4).
+  uint32_t part;
 };
+
+// Partial results of a warp's 32 rows: maxima, sums, outputs (four of dim of each row, then the next)
+template <int D>
+constexpr int64_t part_floats() { return 32 * (D + 2); }
 
 // Whether a phase is over, without waiting (try_wait may sleep until it is)
 __device__ __forceinline__ bool test_wait(uint32_t bar, uint32_t parity) {
@@ -217,6 +234,82 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
                : "memory");
 }
 
+struct Merged {
+  float m, sum;
+  bool last;
+};
+
+// A warp's 32 rows of one part of an item: maxima and sums, outputs in tensor memory.  All but the
+// part that is done last only leave them in memory; that one merges all of them, in the order of the
+// parts, into its own place.  Out of line, for the same reason as wait_on.
+template <int D>
+__device__ __noinline__ Merged merge_parts(float* partial, unsigned* counters, uint32_t code,
+                                           int32_t n_parts, uint32_t t_o, float m, float sum) {
+  const int lane = threadIdx.x & 31;
+  const int32_t at = (int32_t)(code & 0xffff) * kSoftWarps + (threadIdx.x >> 5);
+  constexpr int64_t kNext = kSoftWarps * part_floats<D>();  // on to the next part
+  float* all = partial + at * part_floats<D>();
+  float* mine = all + ((code >> 16) & 15) * kNext;
+  mine[lane] = m;
+  mine[32 + lane] = sum;
+#pragma unroll 1
+  for (int c = 0; c < D / 32; ++c) {
+    uint32_t o[32];
+    tmem_ld_32x32b_x32(t_o + c * 32, o);
+    tmem_ld_wait();
+#pragma unroll
+    for (int v = 0; v < 8; ++v)
+      *reinterpret_cast<uint4*>(mine + 64 + ((c * 8 + v) * 32 + lane) * 4) =
+          make_uint4(o[v * 4], o[v * 4 + 1], o[v * 4 + 2], o[v * 4 + 3]);
+  }
+  __threadfence();
+  __syncwarp();
+  uint32_t done = 0;
+  if (lane == 0) {
+    done = atomicAdd(counters + at, 1u) + 1;
+    if ((int32_t)done == n_parts) counters[at] = 0;  // as the next call finds it
+    __threadfence();
+  }
+  Merged r{m, sum, (int32_t)__shfl_sync(0xffffffffu, done, 0) == n_parts};
+  if (!r.last) return r;
+  float w[kMostParts];
+  r.m = -INFINITY;
+  r.sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kMostParts; ++k) {
+    w[k] = k < n_parts ? __ldcg(all + k * kNext + lane) : -INFINITY;
+    r.m = fmaxf(r.m, w[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kMostParts; ++k) {
+    w[k] = w[k] == -INFINITY ? 0.0f : fast_exp2(w[k] - r.m);
+    if (k < n_parts) r.sum = fmaf(w[k], __ldcg(all + k * kNext + 32 + lane), r.sum);
+  }
+#pragma unroll 1
+  for (int c = 0; c < D / 16; ++c) {
+    const float4* from = reinterpret_cast<const float4*>(all + 64) + c * 4 * 32 + lane;
+    float o[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kMostParts; ++k) {
+      if (k < n_parts) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float4 y = __ldcg(from + k * (kNext / 4) + v * 32);
+          o[v * 4] = fmaf(w[k], y.x, o[v * 4]);
+          o[v * 4 + 1] = fmaf(w[k], y.y, o[v * 4 + 1]);
+          o[v * 4 + 2] = fmaf(w[k], y.z, o[v * 4 + 2]);
+          o[v * 4 + 3] = fmaf(w[k], y.w, o[v * 4 + 3]);
+        }
+      }
+    }
+    tmem_st_32x32b_x16(t_o + c * 16, reinterpret_cast<uint32_t(&)[16]>(o));
+  }
+  tmem_st_wait();
+  return r;
+}
+
 // Pairs of row tiles of request r (0: none, or another kernel's).
 __device__ __forceinline__ int32_t request_pairs(const AttendParams& p, int32_t r, Item& it,
                                                  unsigned* bad) {
@@ -307,7 +400,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
   __syncthreads();
   tc_fence_after();
   if (bad && blockIdx.x == 0) set_error(p.err, bad);
-  const int32_t total = sh.before[kTilesThreads];
+  // Fewer items than CTAs: the tokens of each in parts, whose results the last to be done merges.
+  const int32_t whole = sh.before[kTilesThreads];
+  const int32_t parts = min(kMostParts, max(1, (int32_t)gridDim.x / max(1, whole)));
+  const int32_t total = whole * parts;
   const uint32_t tmem = sh.tmem;
   volatile int* abort = &sh.abort;
   const auto wait = [&](uint64_t* bar, uint32_t phase) {  // a warp goes on, or gives up, as one
@@ -344,15 +440,17 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
           if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
         } else {
           it = Item{};
-          it.more = at < total;
-          if (it.more) {
-            int lo = 0, hi = kTilesThreads;           // the last thread with before <= at
+          do {
+            it.more = at < total;
+            if (!it.more) break;
+            const int32_t of = parts > 1 ? at / parts : at, part = at - of * parts;
+            int lo = 0, hi = kTilesThreads;           // the last thread with before <= of
 #pragma unroll 1
             while (hi - lo > 1) {
               const int mid = (lo + hi) >> 1;
-              if (sh.before[mid] <= at) lo = mid; else hi = mid;
+              if (sh.before[mid] <= of) lo = mid; else hi = mid;
             }
-            int32_t x = at - sh.before[lo], pairs = 0;
+            int32_t x = of - sh.before[lo], pairs = 0;
             int32_t r = per <= 1 ? sh.order[lo] : lo * per;
 #pragma unroll 1
             for (;; ++r) {
@@ -365,8 +463,9 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             it.h = x - back * p.H;
             it.rows0 = max(pairs - 1 - back, 0) * kPairRows;
             const int32_t before_q = it.len - it.n;   // the first query's position
-            if (p.window > 0)
-              it.tile0 = max(0, before_q + attend_query(p, it.rows0) - p.window + 1) / kTileTokens;
+            it.tile0 = p.window > 0
+                           ? max(0, before_q + attend_query(p, it.rows0) - p.window + 1) / kTileTokens
+                           : 0;
             const auto steps = [&](int32_t first) {   // of the tile of rows that begins there
               if (first >= it.rows) return 0;
               const int32_t i1 = min(it.n - 1, attend_query(p, first + kTileRows - 1));
@@ -377,9 +476,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             it.steps0 = steps(it.rows0);
             it.steps1 = steps(it.rows0 + kTileRows);
             it.tiles = max(it.steps0, it.steps1);
+            if (parts > 1) {
+              const int32_t each = max(kLeastSteps, (it.tiles + parts - 1) / parts);
+              it.part = (uint32_t)(of * parts) | (uint32_t)part << 16 |
+                        (uint32_t)((it.steps0 + each - 1) / each) << 20 |
+                        (uint32_t)((it.steps1 + each - 1) / each) << 24;
+              it.steps0 = min(max(it.steps0 - part * each, 0), each);
+              it.steps1 = min(max(it.steps1 - part * each, 0), each);
+              it.tiles = max(it.steps0, it.steps1);
+              it.tile0 += part * each;
+            }
             at = __shfl_sync(0xffffffffu, drawn, 0);
             if (at < total) draw();
-          }
+          } while (it.tiles == 0);                    // (fewer parts than the others have)
           if (items >= kItemRing) ok = wait(&sh.item_empty[slot], items / kItemRing - 1);
           if (lw == 0 && lane == 0 && ok) {
             sh.items[slot] = it;
@@ -529,7 +638,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         if (elect_one()) umma_commit(bar);
         __syncwarp();
       };
-      uint32_t tiles = 0, ns[2] = {0, 0}, nq1 = 0;    // of the CTA; steps of each tile of rows
+      uint32_t tiles = 0, ns[2] = {0, 0}, nq[2] = {0, 0};  // of the CTA; steps, items of each tile of rows
       bool ok = true;
       for (uint32_t items = 0; ok; ++items) {
         const uint32_t slot = items & (kItemRing - 1);
@@ -561,7 +670,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             }
             if (u < mine) {
               if (u == 0) {
-                if (!(ok = wait(&sh.q_full[x], x ? nq1++ : items))) return;
+                if (!(ok = wait(&sh.q_full[x], nq[x]++))) return;
                 tc_fence_after();
               }
               qk(x, st);
@@ -597,13 +706,18 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     // Queries: D / 8 lanes a row, 8 values each, so that a load is of whole rows.  They are copied to
     // their place as they are, while the last step's scores become weights, and become half there.
     constexpr int LR = D / 8, RS = 32 / LR, NQ = 32 / RS;  // lanes of a row, rows of a load, loads
-    Item it{}, next{};
-    const auto output_row = [&](const Item& w, int32_t full) {
-      const int32_t i = attend_query(p, full), j = full - i * p.G;
-      return (int64_t)(w.q0 + i) * (p.H * p.G) + w.h * p.G + j;
+    // Of the item, what its output needs: this tile's first row, all rows, the first one's place
+    // in the output.  (What else there is to know of an item is read from its slot when needed:
+    // registers are few.)
+    int32_t rows0 = 0, rows = 0, place = 0;
+    uint32_t part = 0;
+    const auto output_row = [&](int32_t full) {
+      const int32_t i = attend_query(p, full);
+      return place + i * (p.H * p.G - p.G) + full;  // (the host has seen that 31 bits hold it)
     };
     // The next item with rows of this tile's, if it has been said: the items up to it may have to
     // be done first, and they may need the step that this tile of rows is at.
+    bool more = false;
     const auto take = [&](bool block) {
       for (;;) {
         const uint32_t slot = items & (kItemRing - 1), phase = items / kItemRing;
@@ -613,13 +727,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
                                test_wait(smem_u32(&sh.item_full[slot]), phase & 1u))) {
           return false;
         }
-        next = sh.items[slot];
+        const Item& next = sh.items[slot];
+        more = next.more != 0;
+        if (!more || (x ? next.steps1 : next.steps0) > 0) return true;
+        tiles += next.tiles;
         __syncwarp();
-        if (!next.more) return true;
         if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
         ++items;
-        if ((x ? next.steps1 : next.steps0) > 0) return true;
-        tiles += next.tiles;
       }
     };
     const int q_row = (warp & 3) * 32 + lane / LR, q_chunk = lane % LR;  // of this thread's first load
@@ -629,6 +743,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       return q_line + r * 128 + (((q_chunk ^ r) & 7) << 4);
     };
     const auto fetch = [&]() {
+      const Item& next = sh.items[items & (kItemRing - 1)];
       const int32_t first = min(next.rows0 + x * kTileRows + q_row, next.rows - 1);
       const int32_t left = next.rows - (next.rows0 + x * kTileRows + q_row);
       const int32_t a = attend_query(p, first);
@@ -686,60 +801,77 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     for (;;) {
       if (!known) {
         if (!take(true)) break;
-        if (next.more) fetch();
+        if (more) fetch();
       }
-      if (next.more) put();
+      if (more) put();
 
       if (started) {
         // ---- the output of the item before
-        const int32_t rows0 = it.rows0 + x * kTileRows;
-        const bool none = sum == 0.0f;
-        const float inv = none ? 0.0f : __fdividef(1.0f, sum);
-        if (p.lse && rows0 + row < it.rows)
-          p.lse[output_row(it, rows0 + row)] =
-              none ? -INFINITY : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
         if (!(ok = wait(&sh.o_full[x][1], ns - 1))) break;
         tc_fence_after();
-        // 32 of dim at a time through shared memory: a thread has a row, a store 64 bytes of eight
-        const uint32_t stage = base + L::kOut + warp * 2048;
-        uint16_t* dst[4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int32_t full = rows0 + (warp & 3) * 32 + v * 8 + (lane >> 2);
-          dst[v] = full < it.rows ? p.out + output_row(it, full) * D + (lane & 3) * 8 : nullptr;
+        const int32_t n_parts = (part >> (x ? 24 : 20)) & 15;
+        bool last = true;
+        if (n_parts > 1) {
+          const Merged all = merge_parts<D>(p.tile_partial, p.tile_counters, part, n_parts,
+                                            t_o, m, sum);
+          m = all.m;
+          sum = all.sum;
+          last = all.last;
         }
+        if (last) {
+          const bool none = sum == 0.0f;
+          const float inv = none ? 0.0f : __fdividef(1.0f, sum);
+          if (p.lse && rows0 + row < rows)
+            p.lse[output_row(rows0 + row)] =
+                none ? -INFINITY : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
+          // 32 of dim at a time through shared memory: a thread has a row, a store 64 bytes of eight
+          const uint32_t stage = base + L::kOut + warp * 2048;
+          uint16_t* dst[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int32_t full = rows0 + (warp & 3) * 32 + v * 8 + (lane >> 2);
+            dst[v] =
+                full < rows ? p.out + (int64_t)output_row(full) * D + (lane & 3) * 8 : nullptr;
+          }
 #pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t o[32];
-          tmem_ld_32x32b_x32(t_o + c * 32, o);
-          tmem_ld_wait();
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld_32x32b_x32(t_o + c * 32, o);
+            tmem_ld_wait();
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            uint32_t w[4];
+            for (int v = 0; v < 4; ++v) {
+              uint32_t w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[e] = none ? 0u
-                          : attend_pack2(p.fp16, __uint_as_float(o[v * 8 + 2 * e]) * inv,
-                                         __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
-            sts128(stage + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
+              for (int e = 0; e < 4; ++e)
+                w[e] = none ? 0u
+                            : attend_pack2(p.fp16, __uint_as_float(o[v * 8 + 2 * e]) * inv,
+                                           __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
+              sts128(stage + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const int r = v * 8 + (lane >> 2);
+              const uint4 y = lds128(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+              if (dst[v]) *reinterpret_cast<uint4*>(dst[v] + c * 32) = y;
+            }
+            __syncwarp();
           }
-          __syncwarp();
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const int r = v * 8 + (lane >> 2);
-            const uint4 y = lds128(stage + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
-            if (dst[v]) *reinterpret_cast<uint4*>(dst[v] + c * 32) = y;
-          }
-          __syncwarp();
         }
         tc_fence_before();
       }
-      if (!next.more) break;
-      it = next;
+      if (!more) break;
+      const uint32_t slot = items++ & (kItemRing - 1);
+      const Item it = sh.items[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh.item_empty[slot]);
       started = true;
       known = false;
       const int32_t n_steps = x ? it.steps1 : it.steps0;
-      const int32_t rows0 = it.rows0 + x * kTileRows;
+      rows0 = it.rows0 + x * kTileRows;
+      rows = it.rows;
+      place = it.q0 * (p.H * p.G) + it.h * p.G;
+      part = it.part;
       const int32_t pos = it.len - it.n + attend_query(p, min(rows0 + row, it.rows - 1));
       const int32_t top = p.causal ? min(pos, it.len - 1) : it.len - 1;
       const int32_t bottom = p.window > 0 ? pos - p.window + 1 : 0;
@@ -758,7 +890,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         tc_fence_after();
         if (u + 1 == n_steps) {                       // the last product to read the queries is done
           known = take(false);
-          if (known && next.more) fetch();
+          if (known && more) fetch();
         }
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
@@ -878,9 +1010,9 @@ hs_status launch(const AttendParams& p, cudaStream_t stream) {
                      "kv_attend_tiles shared memory");
   });
   if (st != HS_OK) return st;
-  // At most an item for every pair of tiles that the batch's rows could fill.
+  // At most an item for every pair of tiles that the batch's rows could fill, in parts.
   const int64_t rows = (int64_t)p.n_tokens * p.G;
-  int64_t items = (rows / kPairRows + p.n_req) * p.H;
+  int64_t items = (rows / kPairRows + p.n_req) * p.H * kMostParts;
   if (items > num_sms()) items = num_sms();
   launch_pdl(kv_attend_tiles_kernel<D, FMT>, dim3((unsigned)items), dim3(kTilesThreads), smem,
              stream, p);
@@ -889,6 +1021,12 @@ hs_status launch(const AttendParams& p, cudaStream_t stream) {
 }
 
 }  // namespace
+
+// A CTA has a part of an item, where items have parts.
+size_t tiles_partial_bytes(int32_t dim) {
+  return (size_t)((int64_t)num_sms() * kSoftWarps * 4 *
+                  (dim == 64 ? part_floats<64>() : part_floats<128>()));
+}
 
 hs_status launch_kv_attend_tiles(const AttendParams& p, int32_t dim, int32_t format,
                                  cudaStream_t stream) {

@@ -328,3 +328,44 @@ def test_refusals():
             hs.hs_kv_attend(c, kw.pop("q", q), lens, t, **kw)
         assert e.value.status == status
     hs.hs_get_device_error()
+
+
+SPLIT = {
+    "one": ([3000], [150]),
+    "odd": ([1153, 4097, 515], [130, 161, 515]),
+    "prompt": ([2100], [2100]),
+    "mixed": ([900, 5000, 40, 0, 2600], [1, 290, 40, 3, 333]),
+}
+
+
+@pytest.mark.parametrize("name", sorted(SPLIT))
+@pytest.mark.parametrize("d,H,G,fmt,dtype", [(128, 1, 4, "e4m3", "bf16"), (64, 2, 2, "int8", "fp16"),
+                                             (64, 1, 8, "e4m3", "bf16"), (128, 2, 3, "int8", "bf16")])
+def test_many_rows_of_few_requests(name, d, H, G, fmt, dtype):
+    """Their tokens are shared out; the parts of a pair of tiles of rows differ in number."""
+    lens, n = SPLIT[name]
+    p = problem(lens, n, H, G, d, 32, fmt, dtype)
+    both(p)
+    both(p, window=700)
+    both(p, causal=False)
+    a, b = call(p), call(p)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_parts_that_see_nothing():
+    """More queries than tokens: rows that see nothing beside rows in parts; far scales."""
+    p = problem([700, 2000], [900, 400], 1, 4, 128, 16, "e4m3", "bf16", spread=10)
+    both(p)
+    both(p, window=40)
+
+
+def test_parts_with_nan():
+    """A NaN scale in one part reaches every row that sees its token."""
+    p = problem([3000], [200], 1, 4, 128, 16, "e4m3", "bf16")
+    out, _ = call(p)
+    assert torch.isfinite(out).all()
+    p["cache"].k_scale[p["table"][0, 3].item()] = float("nan")
+    out, _ = call(p)
+    assert torch.isnan(out.float()).all()
+    out, _ = call(p, window=500)
+    assert torch.isfinite(out).all()
