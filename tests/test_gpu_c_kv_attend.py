@@ -369,3 +369,19 @@ def test_parts_with_nan():
     assert torch.isnan(out.float()).all()
     out, _ = call(p, window=500)
     assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("d,H,G,fmt", [(64, 4, 6, "int8"), (128, 1, 4, "e4m3"), (256, 2, 4, "int8")])
+@pytest.mark.parametrize("R,n,most", [(48, 5, 3000), (16, 1, 9000), (100, 2, 1500), (7, 3, 40000)])
+def test_a_piece_for_each_block(d, H, G, fmt, R, n, most):
+    """Fewer (request, head, group)s than the kernel has blocks, but more tokens than those have in
+    one step: lengths that differ much, empty requests and others of no query among them."""
+    rng = np.random.default_rng(R)
+    lens = rng.integers(1, most, size=R)
+    lens[::5] = most
+    lens[3::11] = 0
+    q = np.full(R, n)
+    q[5::9] = 0
+    p = problem(lens.tolist(), q.tolist(), H, G, d, 32, fmt, "bf16")
+    both(p)
+    both(p, window=1024)
