@@ -772,10 +772,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       __syncwarp();
       const uint32_t line = base + L::kQ + x * L::kTileBytes + row * 128;
       uint32_t bits = 0;                            // the row's largest, as in 16 bits without a sign
-#pragma unroll 4
+      uint4 v[LR];
+#pragma unroll
       for (int ch = 0; ch < LR; ++ch) {
-        const uint4 v = lds128(line + (ch >> 3) * L::kBlockBytes + (((ch ^ row) & 7) << 4));
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        v[ch] = lds128(line + (ch >> 3) * L::kBlockBytes + (((ch ^ row) & 7) << 4));
+        const uint32_t w[4] = {v[ch].x, v[ch].y, v[ch].z, v[ch].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           asm("max.u16x2 %0, %0, %1;" : "+r"(bits) : "r"(w[e] & 0x7fff7fffu));
@@ -784,12 +785,12 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       // a power of two of the row's size, kept where it and its inverse are normal
       const uint32_t e = min(max(__float_as_uint(fmaxf(big.x, big.y)) >> 23, 1u), 253u);
       const float by = __uint_as_float((254u - e) << 23);
-#pragma unroll 4
+#pragma unroll
       for (int ch = 0; ch < LR; ++ch) {
-        const uint32_t at = line + (ch >> 3) * L::kBlockBytes + (((ch ^ row) & 7) << 4);
         float f[8];
-        attend_unpack8(lds128(at), p.fp16, f);
-        sts128(at, half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
+        attend_unpack8(v[ch], p.fp16, f);
+        sts128(line + (ch >> 3) * L::kBlockBytes + (((ch ^ row) & 7) << 4),
+               half2_of(f[0] * by, f[1] * by), half2_of(f[2] * by, f[3] * by),
                half2_of(f[4] * by, f[5] * by), half2_of(f[6] * by, f[7] * by));
       }
       qs = __uint_as_float(e << 23) * p.scale_log2;
