@@ -75,10 +75,14 @@ __device__ __forceinline__ bool attend_request(const AttendParams& p, int32_t r,
   return true;
 }
 
+static __device__ __noinline__ int32_t attend_divide(int32_t row, int32_t G) { return row / G; }
+
 // The query that a request's row belongs to: row / G.  With m = ceil(2^32 / G), m * G is less than
-// G over 2^32, so row * m / 2^32 is exact while row * G < 2^32; the host gives m where every row is.
+// G over 2^32, so row * m / 2^32 is exact while row * G < 2^32; the host gives m where every row is
+// and G > 1.  The division itself stands out of line.
 __device__ __forceinline__ int32_t attend_query(const AttendParams& p, int32_t row) {
-  return p.G_inv ? (int32_t)__umulhi((uint32_t)row, p.G_inv) : row / p.G;
+  if (p.G_inv) return (int32_t)__umulhi((uint32_t)row, p.G_inv);
+  return p.G == 1 ? row : attend_divide(row, p.G);
 }
 
 // 8 values of 16 bits that are only 2-byte aligned

@@ -744,25 +744,21 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     };
     const auto fetch = [&]() {
       const Item& next = sh.items[items & (kItemRing - 1)];
-      const int32_t first = min(next.rows0 + x * kTileRows + q_row, next.rows - 1);
-      const int32_t left = next.rows - (next.rows0 + x * kTileRows + q_row);
-      const int32_t a = attend_query(p, first);
-      int32_t b = first - a * p.G;                  // its head of the group
-      const uint16_t* src = p.q + (int64_t)(next.q0 + a) * p.q_token +
-                            (int64_t)(next.h * p.G + b) * p.q_head + q_chunk * 8;
+      const int32_t first = next.rows0 + x * kTileRows + q_row, rows = next.rows;
+      const uint16_t* src = p.q + (int64_t)next.q0 * p.q_token +
+                            (int64_t)(next.h * p.G) * p.q_head + q_chunk * 8;
       const int64_t wrap = p.q_token - (int64_t)p.G * p.q_head;  // on to the next query
-#pragma unroll 2
+#pragma unroll 1
       for (int i = 0; i < NQ; ++i) {
-        const bool in = i * RS < left;
+        const int32_t full = first + i * RS;
+        const bool in = full < rows;
+        const int32_t at = in ? full : 0;
+        const uint16_t* from = src + attend_query(p, at) * wrap + at * p.q_head;
         if (p.q_vec) {
-          cp_async16_zfill(q_place(i), src, in);
+          cp_async16_zfill(q_place(i), from, in);
         } else {
-          const uint4 v = in ? attend_raw8(src) : make_uint4(0u, 0u, 0u, 0u);
+          const uint4 v = in ? attend_raw8(from) : make_uint4(0u, 0u, 0u, 0u);
           sts128(q_place(i), v.x, v.y, v.z, v.w);
-        }
-        if ((i + 1) * RS < left) {                  // to the row after the load's
-          src += RS * p.q_head;
-          for (b += RS; b >= p.G; b -= p.G) src += wrap;
         }
       }
     };
