@@ -123,6 +123,8 @@ struct TilesShared {
   uint64_t p_full[2][2], o_full[2][2];  // ... and half of the tokens
   uint64_t drained;
   Item items[kItemRing];
+  int4 outputs[kSoftWarps];             // what a warp's output needs of its item (registers are few):
+                                        // its tile's first row, rows, the place of row 0, its parts
   float4 scales[kScaleRing][kGroups];   // of 16 tokens: keys', log2 of values', 1 / values'
   uint32_t tmem;
   int abort;
@@ -706,15 +708,6 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     // Queries: D / 8 lanes a row, 8 values each, so that a load is of whole rows.  They are copied to
     // their place as they are, while the last step's scores become weights, and become half there.
     constexpr int LR = D / 8, RS = 32 / LR, NQ = 32 / RS;  // lanes of a row, rows of a load, loads
-    // Of the item, what its output needs: this tile's first row, all rows, the first one's place
-    // in the output.  (What else there is to know of an item is read from its slot when needed:
-    // registers are few.)
-    int32_t rows0 = 0, rows = 0, place = 0;
-    uint32_t part = 0;
-    const auto output_row = [&](int32_t full) {
-      const int32_t i = attend_query(p, full);
-      return place + i * (p.H * p.G - p.G) + full;  // (the host has seen that 31 bits hold it)
-    };
     // The next item with rows of this tile's, if it has been said: the items up to it may have to
     // be done first, and they may need the step that this tile of rows is at.
     bool more = false;
@@ -806,6 +799,14 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         // ---- the output of the item before
         if (!(ok = wait(&sh.o_full[x][1], ns - 1))) break;
         tc_fence_after();
+        __syncwarp();
+        const int4 it = sh.outputs[warp];
+        const int32_t rows0 = it.x, rows = it.y;
+        const uint32_t part = (uint32_t)it.w;
+        const auto output_row = [&](int32_t full) {
+          const int32_t i = attend_query(p, full);
+          return it.z + i * (p.H * p.G - p.G) + full;  // (the host has seen that 31 bits hold it)
+        };
         const int32_t n_parts = (part >> (x ? 24 : 20)) & 15;
         bool last = true;
         if (n_parts > 1) {
@@ -865,10 +866,10 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       started = true;
       known = false;
       const int32_t n_steps = x ? it.steps1 : it.steps0;
-      rows0 = it.rows0 + x * kTileRows;
-      rows = it.rows;
-      place = it.q0 * (p.H * p.G) + it.h * p.G;
-      part = it.part;
+      const int32_t rows0 = it.rows0 + x * kTileRows;
+      if (lane == 0)
+        sh.outputs[warp] =
+            make_int4(rows0, it.rows, it.q0 * (p.H * p.G) + it.h * p.G, (int32_t)it.part);
       const int32_t pos = it.len - it.n + attend_query(p, min(rows0 + row, it.rows - 1));
       const int32_t top = p.causal ? min(pos, it.len - 1) : it.len - 1;
       const int32_t bottom = p.window > 0 ? pos - p.window + 1 : 0;
