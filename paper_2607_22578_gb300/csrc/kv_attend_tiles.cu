@@ -25,8 +25,8 @@
 // of its own; a warp's rows of the parts are merged by the one that is done last (128 queries over
 // 16,384 tokens, 32 / 8 heads of 128: 313 -> 64 us).
 //
-// Measured: 16 prompts of 256 to 2048 tokens, 32 / 8 heads of 128, 347 us (601 TFLOP/s); six chunks of
-// up to 1024 queries behind 1,000 to 12,000 tokens, 32 / 4 heads, 441 (752).  256 rows by 128 tokens
+// Measured: 16 prompts of 256 to 2048 tokens, 32 / 8 heads of 128, 329 us (635 TFLOP/s); six chunks of
+// up to 1024 queries behind 1,000 to 12,000 tokens, 32 / 4 heads, 453 (732).  256 rows by 128 tokens
 // take 4500 clocks, products 2200 of them: the rest is the chain of one tile (scores loaded, maximum,
 // 64 exponentials a thread, twice, then the last product and the next scores).
 //
