@@ -31,10 +31,12 @@
 // 64 exponentials a thread, twice, then the last product and the next scores).
 //
 // Arithmetic: q as half after division by a power of two of its row; codes as half (exact); sums
-// in fp32.  A block's scales enter through the exponent: with c the scores' factor and lv = log2 of
-// the values' scale, p' = 2^(acc * c + lv - m + 7) with m the running maximum of acc * c + lv
-// (it may lag by 8), o = sum p' code, and the weights' sum takes each block's p' / 2^lv.  So value
-// scales may be as far apart as they like.
+// in fp32.  With c a score's factor and vs the values' scale of its block, a row keeps two running
+// maxima (both may lag by 8): ms of the scores s = acc * c, and m of s + log2 vs.  The weights' sum
+// is of z = 2^(s - ms + 7), the output's weights are w = z * vs * 2^(ms - m) as half, o = sum w code,
+// and o * 2^(m - ms) / sum is the output.  With one maximum for both, a block of zeros (scale 2^-126)
+// would drop out of the sum, or overflow it; as it is, a weight is lost where it is below 2^-126 of
+// the row's largest, whatever the scales are.
 #include "kv_attend.cuh"
 #include "kv_cache.cuh"
 
@@ -60,6 +62,7 @@ constexpr int kLeastSteps = 4;                 // of a part
 constexpr float kTilesLag = 8.0f;
 constexpr float kTilesShift = 7.0f;
 constexpr float kLeastScale = 1.17549435e-38f;
+constexpr float kMostFactor = 8.5070592e37f;   // 2^126
 
 template <int D>
 struct TilesLayout {
@@ -83,9 +86,10 @@ struct Item {
   uint32_t part;
 };
 
-// Partial results of a warp's 32 rows: maxima, sums, outputs (four of dim of each row, then the next)
+// Partial results of a warp's 32 rows: both maxima, sums, outputs (four of dim of each row, then the
+// next)
 template <int D>
-constexpr int64_t part_floats() { return 32 * (D + 2); }
+constexpr int64_t part_floats() { return 32 * (D + 3); }
 
 // Whether a phase is over, without waiting (try_wait may sleep until it is)
 __device__ __forceinline__ bool test_wait(uint32_t bar, uint32_t parity) {
@@ -125,7 +129,7 @@ struct TilesShared {
   Item items[kItemRing];
   int4 outputs[kSoftWarps];             // what a warp's output needs of its item (registers are few):
                                         // its tile's first row, rows, the place of row 0, its parts
-  float4 scales[kScaleRing][kGroups];   // of 16 tokens: keys', log2 of values', 1 / values'
+  float4 scales[kScaleRing][kGroups];   // of 16 tokens: keys', log2 of values', values'
   uint32_t tmem;
   int abort;
   int32_t sums[kTilesThreads / 32];
@@ -219,6 +223,11 @@ __device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 
 // The scores' factor; never 0, so that a hidden score's -inf stays one.
 __device__ __forceinline__ float factor(float scale, float q_scale) {
@@ -237,7 +246,7 @@ __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint3
 }
 
 struct Merged {
-  float m, sum;
+  float ms, m, sum;
   bool last;
 };
 
@@ -246,7 +255,8 @@ struct Merged {
 // parts, into its own place.  Out of line, for the same reason as wait_on.
 template <int D>
 __device__ __noinline__ Merged merge_parts(float* partial, unsigned* counters, uint32_t code,
-                                           int32_t n_parts, uint32_t t_o, float m, float sum) {
+                                           int32_t n_parts, uint32_t t_o, float ms, float m,
+                                           float sum) {
   const int lane = threadIdx.x & 31;
   const int32_t at = (int32_t)(code & 0xffff) * kSoftWarps + (threadIdx.x >> 5);
   constexpr int64_t kNext = kSoftWarps * part_floats<D>();  // on to the next part
@@ -254,6 +264,7 @@ __device__ __noinline__ Merged merge_parts(float* partial, unsigned* counters, u
   float* mine = all + ((code >> 16) & 15) * kNext;
   mine[lane] = m;
   mine[32 + lane] = sum;
+  mine[64 + lane] = ms;
 #pragma unroll 1
   for (int c = 0; c < D / 32; ++c) {
     uint32_t o[32];
@@ -261,7 +272,7 @@ __device__ __noinline__ Merged merge_parts(float* partial, unsigned* counters, u
     tmem_ld_wait();
 #pragma unroll
     for (int v = 0; v < 8; ++v)
-      *reinterpret_cast<uint4*>(mine + 64 + ((c * 8 + v) * 32 + lane) * 4) =
+      *reinterpret_cast<uint4*>(mine + 96 + ((c * 8 + v) * 32 + lane) * 4) =
           make_uint4(o[v * 4], o[v * 4 + 1], o[v * 4 + 2], o[v * 4 + 3]);
   }
   __threadfence();
@@ -272,24 +283,29 @@ __device__ __noinline__ Merged merge_parts(float* partial, unsigned* counters, u
     if ((int32_t)done == n_parts) counters[at] = 0;  // as the next call finds it
     __threadfence();
   }
-  Merged r{m, sum, (int32_t)__shfl_sync(0xffffffffu, done, 0) == n_parts};
+  Merged r{ms, m, sum, (int32_t)__shfl_sync(0xffffffffu, done, 0) == n_parts};
   if (!r.last) return r;
+  // the parts' factors: of sums by the scores' maxima, then of outputs by the others
   float w[kMostParts];
-  r.m = -INFINITY;
   r.sum = 0.0f;
 #pragma unroll
-  for (int k = 0; k < kMostParts; ++k) {
-    w[k] = k < n_parts ? __ldcg(all + k * kNext + lane) : -INFINITY;
-    r.m = fmaxf(r.m, w[k]);
-  }
+  for (int y = 0; y < 2; ++y) {
+    float now = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < kMostParts; ++k) {
-    w[k] = w[k] == -INFINITY ? 0.0f : fast_exp2(w[k] - r.m);
-    if (k < n_parts) r.sum = fmaf(w[k], __ldcg(all + k * kNext + 32 + lane), r.sum);
+    for (int k = 0; k < kMostParts; ++k) {
+      w[k] = k < n_parts ? __ldcg(all + k * kNext + (y ? 0 : 64) + lane) : -INFINITY;
+      now = fmaxf(now, w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kMostParts; ++k) {
+      w[k] = w[k] == -INFINITY ? 0.0f : fast_exp2(w[k] - now);
+      if (y == 0 && k < n_parts) r.sum = fmaf(w[k], __ldcg(all + k * kNext + 32 + lane), r.sum);
+    }
+    (y ? r.m : r.ms) = now;
   }
 #pragma unroll 1
   for (int c = 0; c < D / 16; ++c) {
-    const float4* from = reinterpret_cast<const float4*>(all + 64) + c * 4 * 32 + lane;
+    const float4* from = reinterpret_cast<const float4*>(all + 96) + c * 4 * 32 + lane;
     float o[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[e] = 0.0f;
@@ -557,7 +573,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
           const float k = scale.x < kLeastScale ? kLeastScale : scale.x;  // (a NaN stays one)
           const float v = scale.y < kLeastScale ? kLeastScale : scale.y;
           sh.scales[(n - 1) & (kScaleRing - 1)][lane] =
-              make_float4(k, log2f(v), __fdividef(1.0f, v), 0.0f);
+              make_float4(k, log2f(v), scale.y, 0.0f);
         }
         put(base + L::kK + st * L::kTileBytes, kr);
         fence_async_shared();
@@ -787,7 +803,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       mbar_arrive(&sh.q_full[x]);
     };
     bool known = false, started = false;
-    float m = -INFINITY, sum = 0.0f;
+    float ms = -INFINITY, m = -INFINITY, sum = 0.0f;
     for (;;) {
       if (!known) {
         if (!take(true)) break;
@@ -811,17 +827,20 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         bool last = true;
         if (n_parts > 1) {
           const Merged all = merge_parts<D>(p.tile_partial, p.tile_counters, part, n_parts,
-                                            t_o, m, sum);
+                                            t_o, ms, m, sum);
+          ms = all.ms;
           m = all.m;
           sum = all.sum;
           last = all.last;
         }
         if (last) {
           const bool none = sum == 0.0f;
-          const float inv = none ? 0.0f : __fdividef(1.0f, sum);
+          // 2^(m - ms) / sum in two factors, which are in range where the output is
+          const float back = none ? 0.0f : fast_exp2(0.5f * (m - ms));
+          const float inv = none ? 0.0f : __fdividef(back, sum);
           if (p.lse && rows0 + row < rows)
             p.lse[output_row(rows0 + row)] =
-                none ? -INFINITY : (m - kTilesShift + log2f(sum)) * 0.69314718055994531f;
+                none ? -INFINITY : (ms - kTilesShift + log2f(sum)) * 0.69314718055994531f;
           // 32 of dim at a time through shared memory: a thread has a row, a store 64 bytes of eight
           const uint32_t stage = base + L::kOut + warp * 2048;
           uint16_t* dst[4];
@@ -842,8 +861,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 w[e] = none ? 0u
-                            : attend_pack2(p.fp16, __uint_as_float(o[v * 8 + 2 * e]) * inv,
-                                           __uint_as_float(o[v * 8 + 2 * e + 1]) * inv);
+                            : attend_pack2(p.fp16, __uint_as_float(o[v * 8 + 2 * e]) * inv * back,
+                                           __uint_as_float(o[v * 8 + 2 * e + 1]) * inv * back);
               sts128(stage + lane * 64 + ((v ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
             }
             __syncwarp();
@@ -881,7 +900,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       const uint32_t tile_base = tiles;
       tiles += it.tiles;
 
-      m = -INFINITY;
+      ms = m = -INFINITY;
       sum = 0.0f;
       for (int32_t u = 0; u < n_steps; ++u, ++ns) {
         if (!(ok = wait(&sh.s_full[x], ns))) break;
@@ -916,7 +935,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             for (int e = 0; e < kHalfTokens; ++e)
               if (!((e < 32 ? lo : hi) & (1u << (e & 31)))) a[e] = 0xff800000u;  // -inf
           }
-          // ---- the maximum of acc * c + lv
+          // ---- the maxima of s and of s + lv
           float b[kHalfGroups];
 #pragma unroll
           for (int g = 0; g < kHalfGroups; ++g) b[g] = -INFINITY;
@@ -926,14 +945,19 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             for (int g = 0; g < kHalfGroups; ++g)
               b[g] = fmaxf(b[g], fmaxf(__uint_as_float(a[g * 16 + e]),
                                        __uint_as_float(a[g * 16 + e + 1])));
-          float most = -INFINITY;
+          float most = -INFINITY, most_s = -INFINITY;
 #pragma unroll
-          for (int g = 0; g < kHalfGroups; ++g) most = fmaxf(most, fmaf(b[g], by[g], lv[g]));
-          if (__any_sync(0xffffffffu, most > m + kTilesLag)) {
-            const float now = fmaxf(m, most);
+          for (int g = 0; g < kHalfGroups; ++g) {
+            const float s = b[g] * by[g];
+            most_s = fmaxf(most_s, s);
+            most = fmaxf(most, s + lv[g]);
+          }
+          if (__any_sync(0xffffffffu, most > m + kTilesLag || most_s > ms + kTilesLag)) {
+            const float now_s = fmaxf(ms, most_s), now = fmaxf(m, most);
             const float f = m == -INFINITY ? 0.0f : fast_exp2(m - now);
+            if (ms != -INFINITY) sum *= fast_exp2(ms - now_s);
+            ms = now_s;
             m = now;
-            sum *= f;
             if (u > 0 || half > 0) {                  // once the last half's product is done
               if (!(ok = half ? wait(&sh.o_full[x][0], ns) : wait(&sh.o_full[x][1], ns - 1))) break;
               tc_fence_after();
@@ -949,37 +973,36 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             }
           }
           // ---- the weights
-          const float shift = m == -INFINITY ? 0.0f : kTilesShift - m;
-          uint64_t part[kHalfGroups];
-#pragma unroll
-          for (int g = 0; g < kHalfGroups; ++g) part[g] = 0;
+          const float shift = ms == -INFINITY ? 0.0f : kTilesShift - ms;
+          const float root = m == -INFINITY ? 1.0f : fast_exp2(0.5f * (ms - m));
+          const uint64_t shift2 = pack_f32x2(shift, shift);
+          uint64_t part[2] = {0, 0};
 #pragma unroll
           for (int c = 0; c < 2; ++c) {
             uint32_t w[16];
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
               const int g = c * 2 + y;
-              const float add = lv[g] + shift;
-              const uint64_t by2 = pack_f32x2(by[g], by[g]), add2 = pack_f32x2(add, add);
+              // (a group whose tokens have no weight may have a factor out of range)
+              float f = scales[g].z * root * root;
+              f = f > kMostFactor ? kMostFactor : f;
+              const uint64_t by2 = pack_f32x2(by[g], by[g]), f2 = pack_f32x2(f, f);
 #pragma unroll
               for (int e = 0; e < 16; e += 2) {
                 const int k = g * 16 + e;
                 float z0, z1;
-                unpack_f32x2(fma_f32x2(pack_b32x2(a[k], a[k + 1]), by2, add2), z0, z1);
-                z0 = fast_exp2(z0);
-                z1 = fast_exp2(z1);
-                part[g] = add_f32x2(part[g], pack_f32x2(z0, z1));
+                unpack_f32x2(fma_f32x2(pack_b32x2(a[k], a[k + 1]), by2, shift2), z0, z1);
+                const uint64_t z = pack_f32x2(fast_exp2(z0), fast_exp2(z1));
+                part[y] = add_f32x2(part[y], z);
+                unpack_f32x2(mul_f32x2(z, f2), z0, z1);
                 w[y * 8 + e / 2] = half2_of(z0, z1);
               }
             }
             tmem_st_32x32b_x16(t_s + half * 32 + c * 16, w);
           }
-#pragma unroll
-          for (int g = 0; g < kHalfGroups; ++g) {
-            float p0, p1;
-            unpack_f32x2(part[g], p0, p1);
-            sum = fmaf(p0 + p1, scales[g].z, sum);
-          }
+          float p0, p1;
+          unpack_f32x2(add_f32x2(part[0], part[1]), p0, p1);
+          sum += p0 + p1;
           tmem_st_wait();
           tc_fence_before();
           mbar_arrive(&sh.p_full[x][half]);  // (after the second: the scales' place may be written)
