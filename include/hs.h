@@ -728,9 +728,12 @@ hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, i
  * workspace   hs_kv_attend_workspace() bytes, 256-byte aligned, zeroed once
  *             before its first use; every call leaves it fit for the next.
  * Products of 16-bit values with fp32 sums; k and v are exact in them, q but
- * for what is below 2^-24 of its row's largest value, the weights are rounded
- * to half.  Results do not depend on the order in which the kernel's blocks
- * finish.
+ * for what is below 2^-24 of its row's largest value.  The weights times their
+ * block's value scale are rounded to half, to 2^-11 of each or to 2^-32 of the
+ * largest that the query sees, so out is within about 2^-11 of the sum of
+ * weight * |v| beside its own rounding; lse has no such term.  Scales are >= 0,
+ * and may be as far apart as fp32 holds.  Results do not depend on the order in
+ * which the kernel's blocks finish.
  * Slots past a request's end are never read as numbers, whatever they hold.  A
  * NaN or an infinite scale among a request's own tokens is seen by every query
  * that sees the token, and a NaN value of v (its column) also by the queries

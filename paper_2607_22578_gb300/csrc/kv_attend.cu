@@ -23,9 +23,12 @@
 // Measured: 256 requests of 1 to 8192 tokens, 32 / 8 heads of 128, 2.1 GB in 339 to 345 us (0.92 of
 // the copy rate); 8 of 100 to 1500 in 11.6 us, which are launch and round trips; one of 32,771 in 21.2 (67 MB).
 // Arithmetic: q as half after division by a power of two of its row (exact but below 2^-24 of the
-// row's largest), products and sums in fp32, p = 2^(s - m + 7) as half (the running maximum m may
-// lag by 8, so p <= 2^15; what is under 2^-31 of the largest is dropped from o, not from lse),
-// scales of value blocks relative to the largest so far, divided out at the end.
+// row's largest), products and sums in fp32.  A row keeps two running maxima (both may lag by 8): mx
+// of the scores s and mo of s + log2 vs, with vs the values' scale of a token's block.  The weights'
+// sum is of z = 2^(s - mx + 7), the output's weights are w = z * vs * 2^(mx - mo) as half (w <= 2^15;
+// what is under 2^-32 of a row's largest is dropped from o, not from lse), and o * 2^(mo - mx) / sum is
+// the output.  So a block counts by what its values weigh in that row, not by its scale: one that a
+// row does not see, or hardly, takes no bits from the others.
 #include <algorithm>
 
 #include "kv_cache.cuh"
@@ -46,6 +49,8 @@ constexpr int kAttStages = 2;
 constexpr int kSpareBytes = 25000000;
 constexpr float kLag = 8.0f;                             // of the running maximum, in powers of two
 constexpr float kShift = 7.0f;
+constexpr float kLeastScale = 1.17549435e-38f;           // 2^-126
+constexpr float kMostFactor = 8.5070592e37f;             // 2^126
 
 // Warps of a CTA, and CTAs of an SM.  Small CTAs side by side go on loading while one of them ends
 // a (request, head, group), a single large one leaves few parts of a long one to merge.  8 of 16,000
@@ -156,7 +161,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
   constexpr int NO = HALVES * KS * NT * 4;       // output registers of a thread
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int32_t last_s;
-  __shared__ float m_s[WARPS][ROWS];
+  __shared__ float mx_s[WARPS][ROWS], mo_s[WARPS][ROWS];
 
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, c = lane & 3;
@@ -374,7 +379,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
 
   uint32_t qf[HALVES][KS][NT][2];
   float o[HALVES][KS][NT][4];
-  float mx[NT][2], sum[NT][2], qs[NT][2];
+  float mx[NT][2], mo[NT][2], sum[NT][2], qs[NT][2];
   int32_t top[NT][2], bottom[NT][2];                      // keys that a row sees: bottom .. top
   // A place's queries as they are stored; a thread has row g of each eight, 4 of dim a k16 step.
   const auto load_queries = [&](const Place& w) {
@@ -408,7 +413,6 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
 #pragma unroll
   for (int x = 0; x < 2; ++x)
     v_lane[x] = D == 64 ? chunk_at<D>(2 * c + x, g >> 1) + (g & 1) * 8 : chunk_at<D>(2 * c + x, g);
-  float v_ref = 0.0f;
   bool fresh = true;
   int32_t seg_tile = 0;                                   // the first tile that this CTA has of it
   Place at{}, next{};                                     // what is computed, what was loaded last
@@ -450,7 +454,6 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       if (fresh) {                                          // a (request, head, group) begins
         fresh = false;
         seg_tile = at.tile;
-        v_ref = 1.17549435e-38f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float big = 0.0f;
@@ -481,7 +484,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             qs[nt][e] = __shfl_sync(0xffffffffu, back, (2 * c + e) * 4);
-            mx[nt][e] = -INFINITY;
+            mx[nt][e] = mo[nt][e] = -INFINITY;
             sum[nt][e] = 0.0f;
             const int pos = at.len - at.n + attend_query(p, at.group * ROWS + nt * 8 + 2 * c + e);
             top[nt][e] = p.causal ? min(pos, at.len - 1) : at.len - 1;
@@ -542,17 +545,20 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             }
           }
         }
-        // ---- masks, running maximum
+        // ---- masks, running maxima
         const bool whole = t0 + kWarpTokens <= (p.causal ? at.len - at.n + 1 : at.len) &&
                            (p.window <= 0 || t0 > at.len - 1 - p.window);
-        float most[NT][2];
+        const float lv[2] = {__log2f(fmaxf(scales[2], kLeastScale)),
+                             __log2f(fmaxf(scales[3], kLeastScale))};
+        float most[NT][2], most_o[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float m = -INFINITY;
+            most[nt][e] = most_o[nt][e] = -INFINITY;
 #pragma unroll
-            for (int mt = 0; mt < 2; ++mt)
+            for (int mt = 0; mt < 2; ++mt) {
+              float m = -INFINITY;
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 float& z = s[mt][nt][2 * x + e];
@@ -563,55 +569,67 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
                 }
                 m = fmaxf(m, z);
               }
-            most[nt][e] = m;
+              most[nt][e] = fmaxf(most[nt][e], m);
+              most_o[nt][e] = fmaxf(most_o[nt][e], m + lv[mt]);
+            }
           }
         bool grow = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) grow |= most[nt][e] > mx[nt][e] + kLag;
-        const float v_top = fmaxf(v_ref, fmaxf(scales[2], scales[3]));
-        const bool v_grow = v_top > v_ref;
-        if (__any_sync(0xffffffffu, grow || v_grow)) {
-          const float vr = v_grow ? __fdividef(v_ref, v_top) : 1.0f;
-          v_ref = v_top;
+          for (int e = 0; e < 2; ++e)
+            grow |= most[nt][e] > mx[nt][e] + kLag || most_o[nt][e] > mo[nt][e] + kLag;
+        if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float m = most[nt][e];
+              float m = most[nt][e], n = most_o[nt][e];
 #pragma unroll
-              for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+              for (int x = 4; x < 32; x <<= 1) {
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+                n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, x));
+              }
               m = fmaxf(m, mx[nt][e]);
-              const float f = m == -INFINITY ? 1.0f : fast_exp2(mx[nt][e] - m);
+              n = fmaxf(n, mo[nt][e]);
+              sum[nt][e] *= m == -INFINITY ? 1.0f : fast_exp2(mx[nt][e] - m);
+              const float f = n == -INFINITY ? 1.0f : fast_exp2(mo[nt][e] - n);
               mx[nt][e] = m;
-              sum[nt][e] *= f;
+              mo[nt][e] = n;
 #pragma unroll
               for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
-                  o[hf][k][nt][e] *= f * vr;
-                  o[hf][k][nt][2 + e] *= f * vr;
+                  o[hf][k][nt][e] *= f;
+                  o[hf][k][nt][2 + e] *= f;
                 }
             }
         }
-        // ---- p = 2^(s - m + 7), and o += p . v with dim as M, rows as N, tokens as K
-        const float inv_ref = __fdividef(1.0f, v_ref);
+        // ---- the weights, and o += w . v with dim as M, rows as N, tokens as K
+        float root[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+            root[nt][e] = mo[nt][e] == -INFINITY ? 1.0f
+                                                 : fast_exp2(0.5f * (mx[nt][e] - mo[nt][e]));
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
-          const float ratio = scales[2 + mt] * inv_ref;
           uint32_t pb[NT][2];
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const float m = mx[nt][e] == -INFINITY ? 0.0f : mx[nt][e] - kShift;
+              // (where no token has weight, it may be out of range)
+              float f = scales[2 + mt] * root[nt][e] * root[nt][e];
+              f = f > kMostFactor ? kMostFactor : f;
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 float& z = s[mt][nt][2 * x + e];
                 z = fast_exp2(z - m);
                 sum[nt][e] += z;
-                z *= ratio;
+                z *= f;
               }
             }
             pb[nt][0] = transpose_8x8(pack_half2(s[mt][nt][0], s[mt][nt][1]));
@@ -667,26 +685,32 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1)
           sum[nt][e] += __shfl_xor_sync(0xffffffffu, sum[nt][e], x);
-        if (g == 0) m_s[warp][nt * 8 + 2 * c + e] = mx[nt][e];
+        if (g == 0) {
+          mx_s[warp][nt * 8 + 2 * c + e] = mx[nt][e];
+          mo_s[warp][nt * 8 + 2 * c + e] = mo[nt][e];
+        }
       }
     __syncthreads();
-    float big[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float m = -INFINITY;
+        float m = -INFINITY, n = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) m = fmaxf(m, m_s[w][nt * 8 + 2 * c + e]);
-        big[nt][e] = m;
-        const float f = mx[nt][e] == -INFINITY ? 0.0f : fast_exp2(mx[nt][e] - m);
-        sum[nt][e] *= f;
+        for (int w = 0; w < WARPS; ++w) {
+          m = fmaxf(m, mx_s[w][nt * 8 + 2 * c + e]);
+          n = fmaxf(n, mo_s[w][nt * 8 + 2 * c + e]);
+        }
+        sum[nt][e] *= mx[nt][e] == -INFINITY ? 0.0f : fast_exp2(mx[nt][e] - m);
+        const float f = mo[nt][e] == -INFINITY ? 0.0f : fast_exp2(mo[nt][e] - n);
+        mx[nt][e] = m;                                      // of the CTA from here on
+        mo[nt][e] = n;
 #pragma unroll
         for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
           for (int k = 0; k < KS; ++k) {
-            o[hf][k][nt][e] *= f * v_ref;
-            o[hf][k][nt][2 + e] *= f * v_ref;
+            o[hf][k][nt][e] *= f;
+            o[hf][k][nt][2 + e] *= f;
           }
       }
 #pragma unroll 1
@@ -722,7 +746,9 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
           const int64_t r = (int64_t)(done.q0 + i) * (p.H * p.G) + done.h * p.G + j;
           const float l = sum[nt][e];
           const bool none = l == 0.0f;
-          const float inv = none ? 0.0f : __fdividef(1.0f, l);
+          // 2^(mo - mx) / sum in two factors, which are in range where the output is
+          const float back = none ? 0.0f : fast_exp2(0.5f * (mo[nt][e] - mx[nt][e]));
+          const float inv = none ? 0.0f : __fdividef(back, l);
 #pragma unroll
           for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
@@ -731,25 +757,25 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
 #pragma unroll
               for (int q = 0; q < 4; ++q)
                 w[q] = none ? 0u
-                            : attend_pack2(p.fp16, o[hf][k + q][nt][e] * inv,
-                                           o[hf][k + q][nt][2 + e] * inv);
+                            : attend_pack2(p.fp16, o[hf][k + q][nt][e] * inv * back,
+                                           o[hf][k + q][nt][2 + e] * inv * back);
               *reinterpret_cast<uint4*>(p.out + r * D + hf * 128 + g * (2 * KS) + 2 * k) =
                   make_uint4(w[0], w[1], w[2], w[3]);
             }
           if (g == 0 && p.lse)
-            p.lse[r] = none ? -INFINITY : (big[nt][e] - kShift + log2f(l)) * 0.69314718055994531f;
+            p.lse[r] = none ? -INFINITY : (mx[nt][e] - kShift + log2f(l)) * 0.69314718055994531f;
         }
     };
     if (all_of_it) {
       if (warp == 0) write();
     } else {
       // Partial results: the part that begins at this CTA's first unit in its slot 0, one that
-      // begins later (and so runs past its last) in slot 1.  A slot is its rows' maxima, their
-      // sums, and the sums of weighted values [row][dim].
+      // begins later (and so runs past its last) in slot 1.  A slot is its rows' mx, their sums, their
+      // mo, and the sums of weighted values [row][dim].
       const int64_t first = u_begin + i - 1 - (done.tile - done.tile0);   // units of the whole
       const int64_t last = first + (done.tile_end - done.tile0) - 1;
       const int32_t c0 = cta_of(first), c1 = cta_of(last);
-      constexpr int PS = ROWS * (D + 2);
+      constexpr int PS = ROWS * (D + 3);
       const int32_t odd = first > begins(c0) ? 1 : 0;                  // the first part's slot
       const auto slot_of = [&](int32_t k) {                           // of part k
         return p.partial + ((int64_t)(c0 + k) * 2 + (k == 0 ? odd : 0)) * PS;
@@ -762,14 +788,15 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
           for (int e = 0; e < 2; ++e) {
             const int row = nt * 8 + 2 * c + e;
             if (g == 0) {
-              __stcg(d + row, big[nt][e]);
+              __stcg(d + row, mx[nt][e]);
               __stcg(d + ROWS + row, sum[nt][e]);
+              __stcg(d + 2 * ROWS + row, mo[nt][e]);
             }
 #pragma unroll
             for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
               for (int k = 0; k < KS; k += 2)
-                __stcg(reinterpret_cast<float4*>(d + 2 * ROWS + row * D + hf * 128 +
+                __stcg(reinterpret_cast<float4*>(d + 3 * ROWS + row * D + hf * 128 +
                                                  g * (2 * KS) + 2 * k),
                        make_float4(o[hf][k][nt][e], o[hf][k][nt][2 + e], o[hf][k + 1][nt][e],
                                    o[hf][k + 1][nt][2 + e]));
@@ -784,18 +811,18 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
         const int32_t parts = c1 - c0 + 1;
         // A thread has NF times four values, THREADS apart; UN parts of them on their way at once.
         constexpr int NF = (ROWS * D / 4 + THREADS - 1) / THREADS;
-        constexpr int UN = NF >= 4 ? 2 : NF >= 2 ? 4 : 10;
+        constexpr int UN = NF >= 4 ? 1 : NF >= 2 ? 3 : 9;
         float4 acc[NF];
-        float m[NF], l[NF];
+        float m[NF], mo[NF], l[NF];
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
           acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          m[i] = -INFINITY;
+          m[i] = mo[i] = -INFINITY;
           l[i] = 0.0f;
         }
         for (int32_t k0 = 0; k0 < parts; k0 += UN) {
           float4 v[NF][UN];
-          float pm[NF][UN], pl[NF][UN];
+          float pm[NF][UN], po[NF][UN], pl[NF][UN];
 #pragma unroll
           for (int y = 0; y < UN; ++y) {
             const bool in = k0 + y < parts;
@@ -805,25 +832,30 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
               const int f = min(tid + i * THREADS, ROWS * D / 4 - 1), row = f / (D / 4);
               pm[i][y] = in ? __ldcg(d + row) : -INFINITY;
               pl[i][y] = __ldcg(d + ROWS + row);
-              v[i][y] = __ldcg(reinterpret_cast<const float4*>(d + 2 * ROWS) + f);
+              po[i][y] = in ? __ldcg(d + 2 * ROWS + row) : -INFINITY;
+              v[i][y] = __ldcg(reinterpret_cast<const float4*>(d + 3 * ROWS) + f);
             }
           }
 #pragma unroll
           for (int i = 0; i < NF; ++i) {
-            float now = m[i];
+            float now = m[i], now_o = mo[i];
 #pragma unroll
-            for (int y = 0; y < UN; ++y) now = fmaxf(now, pm[i][y]);
-            const float back = m[i] == -INFINITY ? 0.0f : fast_exp2(m[i] - now);
+            for (int y = 0; y < UN; ++y) {
+              now = fmaxf(now, pm[i][y]);
+              now_o = fmaxf(now_o, po[i][y]);
+            }
+            const float back = mo[i] == -INFINITY ? 0.0f : fast_exp2(mo[i] - now_o);
+            l[i] *= m[i] == -INFINITY ? 0.0f : fast_exp2(m[i] - now);
             m[i] = now;
-            l[i] *= back;
+            mo[i] = now_o;
             acc[i].x *= back;
             acc[i].y *= back;
             acc[i].z *= back;
             acc[i].w *= back;
 #pragma unroll
             for (int y = 0; y < UN; ++y) {
-              const float w = pm[i][y] == -INFINITY ? 0.0f : fast_exp2(pm[i][y] - now);
-              l[i] = fmaf(w, pl[i][y], l[i]);
+              if (pm[i][y] != -INFINITY) l[i] = fmaf(fast_exp2(pm[i][y] - now), pl[i][y], l[i]);
+              const float w = po[i][y] == -INFINITY ? 0.0f : fast_exp2(po[i][y] - now_o);
               acc[i].x = fmaf(w, v[i][y].x, acc[i].x);
               acc[i].y = fmaf(w, v[i][y].y, acc[i].y);
               acc[i].z = fmaf(w, v[i][y].z, acc[i].z);
@@ -838,11 +870,12 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
           const int a = attend_query(p, full), b = full - a * p.G;
           const int64_t r = (int64_t)(done.q0 + a) * (p.H * p.G) + done.h * p.G + b;
           const bool none = l[i] == 0.0f;
-          const float inv = none ? 0.0f : __fdividef(1.0f, l[i]);
+          const float back = none ? 0.0f : fast_exp2(0.5f * (mo[i] - m[i]));
+          const float inv = none ? 0.0f : __fdividef(back, l[i]);
           uint2 w = make_uint2(0u, 0u);
           if (!none) {
-            w.x = attend_pack2(p.fp16, acc[i].x * inv, acc[i].y * inv);
-            w.y = attend_pack2(p.fp16, acc[i].z * inv, acc[i].w * inv);
+            w.x = attend_pack2(p.fp16, acc[i].x * inv * back, acc[i].y * inv * back);
+            w.y = attend_pack2(p.fp16, acc[i].z * inv * back, acc[i].w * inv * back);
           }
           *reinterpret_cast<uint2*>(p.out + r * D + (f - row * (D / 4)) * 4) = w;
           if (f == row * (D / 4) && p.lse)
@@ -923,7 +956,7 @@ static int32_t few_rows(const AttendParams& p) {
 static size_t few_partial_bytes(int32_t dim) {
   const int64_t rows = dim == 64 ? 32 : 16;               // of a tile, at most
   const int64_t ctas = (int64_t)num_sms() * kAttendMaxPerSm;
-  return (size_t)(ctas * 2 * rows * (dim + 2) * 4);
+  return (size_t)(ctas * 2 * rows * (dim + 3) * 4);
 }
 
 // `rows`: of a request, at most

@@ -50,3 +50,48 @@ def wild(lens, n, H, G, d, bt, fmt, spread, seed=1):
 def test_scales_far_apart_many_rows(shape, d, fmt, spread):
     lens, n = SHAPES[shape]
     far.check(wild(lens, n, 2, 4, d, 16, fmt, spread))
+
+
+@pytest.mark.parametrize("lens,n", [([300, 129, 700], [1, 1, 1]), ([900], [7]), ([9000, 40], [1, 3])])
+@pytest.mark.parametrize("d,fmt", [(64, "int8"), (128, "e4m3"), (256, "e4m3")])
+@pytest.mark.parametrize("spread", [30, 100])
+def test_scales_far_apart_few_rows(lens, n, d, fmt, spread):
+    far.check(wild(lens, n, 2, 4, d, 16, fmt, spread))
+
+
+@pytest.mark.parametrize("n", [4, 8, 160])
+@pytest.mark.parametrize("d,fmt", [(64, "int8"), (128, "e4m3"), (256, "int8")])
+@pytest.mark.parametrize("up", [28, 32, 90])
+def test_a_far_larger_block_that_is_hidden(n, d, fmt, up):
+    """The last block is 2^up times the others; its tokens are the last four, which the queries
+    before them do not see, nor any query with a window those of the first block."""
+    p = far.written([324], [n], 2, 4, d, 16, fmt, "bf16", lambda v, r, pos: v)
+    p["cache"].v_scale[p["table"][0, -1].long()] *= 2.0 ** up
+    far.check(p)
+    p["cache"].v_scale[p["table"][0, 0].long()] *= 2.0 ** up
+    far.check(p, window=120)
+
+
+@pytest.mark.parametrize("n", [1, 160])
+@pytest.mark.parametrize("d,fmt", [(64, "int8"), (128, "e4m3"), (256, "int8")])
+@pytest.mark.parametrize("up", [28, 32, 60])
+def test_a_far_larger_block_of_no_weight(n, d, fmt, up):
+    """Every query sees the block that is 2^up times the others, under a score 300 below theirs."""
+    p = far.written([400, 90], [n, min(n, 90)], 2, 4, d, 16, fmt, "bf16", lambda v, r, pos: v)
+    p["q"].abs_().clamp_(min=0.25)
+    c = p["cache"]
+    for r in range(2):
+        b = p["table"][r, 1].long()
+        c.k.view(torch.uint8)[b] = 0xF8 if fmt == "e4m3" else 256 - 64       # -256, -64
+        c.k_scale[b] = 300 / (0.25 * (256 if fmt == "e4m3" else 64) * d ** 0.5)
+        c.v_scale[b] *= 2.0 ** up
+    far.check(p)
+
+
+@pytest.mark.parametrize("n", [1, 160])
+@pytest.mark.parametrize("up", [119, -125])
+def test_ends_of_the_range(n, up):
+    """Values near the largest and the smallest numbers of bf16."""
+    p = far.written([400, 90], [n, min(n, 90)], 2, 4, 128, 16, "e4m3", "bf16", lambda v, r, pos: v)
+    p["cache"].v_scale.fill_(2.0 ** up)
+    far.check(p)
