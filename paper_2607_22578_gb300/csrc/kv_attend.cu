@@ -545,6 +545,18 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             }
           }
         }
+        // Scales that are no number: see below
+        int odd = 0;
+        if (!((scales[0] * 0.0f + scales[1] * 0.0f) + (scales[2] * 0.0f + scales[3] * 0.0f) == 0.0f)) {
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt) {
+            if (!(scales[mt] < INFINITY)) scales[mt] = __int_as_float(0x7fffffff);
+            if (!(scales[2 + mt] < INFINITY)) {
+              scales[2 + mt] = 0.0f;
+              odd |= 1 << mt;
+            }
+          }
+        }
         // ---- masks, running maxima
         const bool whole = t0 + kWarpTokens <= (p.causal ? at.len - at.n + 1 : at.len) &&
                            (p.window <= 0 || t0 > at.len - 1 - p.window);
@@ -604,6 +616,19 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
                   o[hf][k][nt][2 + e] *= f;
                 }
             }
+        }
+        // A value scale that is no number, for the rows that see one of its tokens: a maximum that is
+        // none either makes their weights NaN.  (A key's makes their scores so.)
+        if (odd) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+#pragma unroll
+              for (int mt = 0; mt < 2; ++mt)
+                if ((odd >> mt & 1) && max(t0 + mt * 16, bottom[nt][e]) <=
+                                           min(t0 + mt * 16 + 15, top[nt][e]))
+                  mo[nt][e] = __int_as_float(0x7fffffff);
         }
         // ---- the weights, and o += w . v with dim as M, rows as N, tokens as K
         float root[NT][2];
@@ -854,7 +879,8 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             acc[i].w *= back;
 #pragma unroll
             for (int y = 0; y < UN; ++y) {
-              if (pm[i][y] != -INFINITY) l[i] = fmaf(fast_exp2(pm[i][y] - now), pl[i][y], l[i]);
+              // (a part without a maximum may have a NaN for a sum, and 0 times that is one)
+              l[i] = fmaf(pm[i][y] == -INFINITY ? 0.0f : fast_exp2(pm[i][y] - now), pl[i][y], l[i]);
               const float w = po[i][y] == -INFINITY ? 0.0f : fast_exp2(po[i][y] - now_o);
               acc[i].x = fmaf(w, v[i][y].x, acc[i].x);
               acc[i].y = fmaf(w, v[i][y].y, acc[i].y);

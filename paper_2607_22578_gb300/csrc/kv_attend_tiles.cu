@@ -129,7 +129,8 @@ struct TilesShared {
   Item items[kItemRing];
   int4 outputs[kSoftWarps];             // what a warp's output needs of its item (registers are few):
                                         // its tile's first row, rows, the place of row 0, its parts
-  float4 scales[kScaleRing][kGroups];   // of 16 tokens: keys', log2 of values', values'
+  // of 16 tokens: keys', log2 of values' (always a number), values'; NaN for what is no number
+  float4 scales[kScaleRing][kGroups];
   uint32_t tmem;
   int abort;
   int32_t sums[kTilesThreads / 32];
@@ -570,10 +571,11 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
       if (fetched) {
         if (n > 2 && !(ok = wait(&sh.k_empty[st], use - 1))) break;
         if (lw == 0 && lane < kGroups) {
-          const float k = scale.x < kLeastScale ? kLeastScale : scale.x;  // (a NaN stays one)
-          const float v = scale.y < kLeastScale ? kLeastScale : scale.y;
+          const bool k = scale.x < INFINITY, v = scale.y < INFINITY;    // (a NaN is not)
           sh.scales[(n - 1) & (kScaleRing - 1)][lane] =
-              make_float4(k, log2f(v), scale.y, 0.0f);
+              make_float4(k ? fmaxf(scale.x, kLeastScale) : __int_as_float(0x7fffffff),
+                          v ? log2f(fmaxf(scale.y, kLeastScale)) : 0.0f,
+                          v ? scale.y : __int_as_float(0x7fffffff), 0.0f);
         }
         put(base + L::kK + st * L::kTileBytes, kr);
         fence_async_shared();
@@ -925,6 +927,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             lv[g] = scales[g].y;
           }
           tmem_ld_wait();
+          uint32_t hidden = 0;                        // groups of which this row sees no token
           if (t0 < from || t0 + kHalfTokens - 1 > to) {
             // a bit for each token that is seen
             const int32_t last = min(max(top - t0, -1), kHalfTokens - 1);
@@ -934,6 +937,13 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
 #pragma unroll
             for (int e = 0; e < kHalfTokens; ++e)
               if (!((e < 32 ? lo : hi) & (1u << (e & 31)))) a[e] = 0xff800000u;  // -inf
+            // a scale that is no number is not theirs (where they see a token, it is)
+#pragma unroll
+            for (int g = 0; g < kHalfGroups; ++g)
+              if (!((g < 2 ? lo : hi) & (0xffffu << (g & 1) * 16))) {
+                by[g] = 1.0f;
+                hidden |= 1u << g;
+              }
           }
           // ---- the maxima of s and of s + lv
           float b[kHalfGroups];
@@ -985,7 +995,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
               const int g = c * 2 + y;
               // (a group whose tokens have no weight may have a factor out of range)
               float f = scales[g].z * root * root;
-              f = f > kMostFactor ? kMostFactor : f;
+              f = hidden & (1u << g) ? 0.0f : f > kMostFactor ? kMostFactor : f;
               const uint64_t by2 = pack_f32x2(by[g], by[g]), f2 = pack_f32x2(f, f);
 #pragma unroll
               for (int e = 0; e < 16; e += 2) {

@@ -95,3 +95,44 @@ def test_ends_of_the_range(n, up):
     p = far.written([400, 90], [n, min(n, 90)], 2, 4, 128, 16, "e4m3", "bf16", lambda v, r, pos: v)
     p["cache"].v_scale.fill_(2.0 ** up)
     far.check(p)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("n", [1, 7, 160, 300])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("what", ["k_scale", "v_scale"])
+def test_scales_that_are_no_number(what, d, n, value):
+    """Queries that see a token of such a block get NaN, the others what they see: those before it,
+    and those whose window has left it behind."""
+    p = far.written([333, 333], [n, n], 2, 4, d, 16, "e4m3", "bf16", lambda v, r, pos: v)
+    L, bad = 333, torch.zeros(333, dtype=torch.bool, device="cuda")
+    bad[20 * 16:21 * 16] = True                          # the last block but one of the first request
+    bad[9 * 16:10 * 16] = True
+    for window in (0, 150, 330):
+        want = far.attend(p, window=window)
+        t = getattr(p["cache"], what)
+        keep = t.clone()
+        t[p["table"][0, [9, 20]].long(), 1] = value      # of the second kv head
+        got = far.call(p, window=window)
+        hs.hs_get_device_error()
+        t.copy_(keep)
+        hit = torch.zeros(got[1].shape, dtype=torch.bool, device="cuda")
+        hit[:n, 4:] = (far.sees(L, n, True, window) & bad).any(1)[:, None]
+        assert torch.isnan(got[0][hit].float()).all()
+        assert torch.isnan(got[1][hit]).all() or what == "v_scale"
+        far.compare(got, want, rows=~hit)
+
+
+@pytest.mark.parametrize("n,L", [(1, 9000), (5, 300), (160, 700), (300, 333)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_keys_that_are_no_number_everywhere(d, n, L):
+    """Every row of such a request is NaN, in each of its parts; the next one is not touched."""
+    p = far.written([L, 333], [n, n], 2, 4, d, 16, "e4m3", "bf16", lambda v, r, pos: v)
+    want = far.attend(p)
+    p["cache"].k_scale[p["table"][0, :-(-L // 16)].long()] = float("nan")
+    got = far.call(p)
+    hs.hs_get_device_error()
+    assert torch.isnan(got[0][:n].float()).all() and torch.isnan(got[1][:n]).all()
+    rows = torch.zeros(got[1].shape, dtype=torch.bool, device="cuda")
+    rows[n:] = True
+    far.compare(got, want, rows=rows)
