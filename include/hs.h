@@ -734,10 +734,11 @@ hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, i
  * weight * |v| beside its own rounding; lse has no such term.  Scales are >= 0,
  * and may be as far apart as fp32 holds.  Results do not depend on the order in
  * which the kernel's blocks finish.
- * Slots past a request's end are never read as numbers, whatever they hold.  A
- * NaN or an infinite scale makes NaN of the outputs (the keys' also of lse) of
- * the queries that see a token of its block, and of no other.  A NaN value of v
- * may reach its column of any query of the same call and request, seen or not.
+ * Slots past a request's end, and tokens that the windows of all its queries
+ * have left behind, are never read as numbers, whatever they hold.  A NaN or an
+ * infinite scale makes NaN of the outputs (the keys' also of lse) of the queries
+ * that see a token of its block, and of no other.  A NaN value of v that one
+ * query of a request sees may reach its column of the others of that call too.
  * Device errors (HS_ERR_INVALID_ARG in the error word): starts or lens that
  * cannot be (the request's rows are left as they were), a table entry that is
  * no block (its tokens count as zeros).

@@ -15,8 +15,9 @@
 //    and the one that comes last merges them in their order: no second launch, and a result that
 //    does not depend on which was last.
 //  - A warp takes 32 of a unit's tokens through a ring of its own in shared memory (cp.async,
-//    codes and scales, tokens past the end as zeros, so what stale slots hold is never read) and
-//    keeps its own running maximum and sum: no barrier until a (request, head, group) ends.
+//    codes and scales, tokens past the end and before all windows as zeros, so what stale slots hold
+//    is never read) and keeps its own running maxima and sum: no barrier until a (request, head, group)
+//    ends.
 //  - Products are on mma.sync m16n8k16 with tokens as M and rows as N: a decoding step has 1 to 16
 //    rows, which would fill an eighth of a tcgen05 tile's 128, and codes go straight from shared
 //    memory to registers as half2 (exact for e4m3 and int8).
@@ -136,7 +137,7 @@ __device__ __forceinline__ void divide(const AttendParams& p, Request& q) {
   q.groups = q.tile0 = q.tiles = 0;
   if (q.n == 0 || q.n * p.G > p.rows_most) return;
   q.groups = (q.n * p.G + ROWS - 1) / ROWS;
-  if (p.window > 0) q.tile0 = max(q.len - q.n - p.window + 1, 0) / TOKENS;
+  q.tile0 = attend_first(p, q.n, q.len) / TOKENS;
   q.tiles = max((q.len + TOKENS - 1) / TOKENS - q.tile0, 1);  // an empty one too
 }
 
@@ -352,13 +353,14 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       // rows past the end are zeros (their addresses are inside the block all the same).
       constexpr int CH = D / 16, RPI = 32 / CH;           // chunks of a row, rows of a copy
       const int r0 = lane / CH;
+      const int32_t from = attend_first(p, fetch.n, fetch.len) - t0;  // rows before it are zeros too
       const uint8_t* k0 = p.k + b0 + lane * 16;
       const uint8_t* v0 = p.v + b0 + lane * 16;
       const int64_t other = b1 - b0;                      // of the second 16 tokens
       const uint32_t dst = base + chunk_at<D>(r0, lane % CH);
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const bool ok = r0 < left - i * RPI;
+        const bool ok = r0 < left - i * RPI && r0 >= from - i * RPI;
         const int64_t off = i * 512 + (i < CH / 2 ? 0 : other);
         const uint32_t to = (dst + i * 512) ^ (D == 64 ? 0 : ((i * RPI) & 7) << 4);
         cp_async16_zfill(to, k0 + off, ok);

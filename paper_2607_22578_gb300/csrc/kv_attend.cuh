@@ -75,6 +75,12 @@ __device__ __forceinline__ bool attend_request(const AttendParams& p, int32_t r,
   return true;
 }
 
+// The first token that a query of a request sees.  What is before it is loaded as zeros: a weight of 0
+// would not keep a NaN among its values from the outputs.
+__device__ __forceinline__ int32_t attend_first(const AttendParams& p, int32_t n, int32_t len) {
+  return p.window > 0 ? max(len - n - p.window + 1, 0) : 0;
+}
+
 static __device__ __noinline__ int32_t attend_divide(int32_t row, int32_t G) { return row / G; }
 
 // The query that a request's row belongs to: row / G.  With m = ceil(2^32 / G), m * G is less than

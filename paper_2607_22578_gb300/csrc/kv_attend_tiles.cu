@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
     draw();
     uint32_t items = 0;                             // said so far
     bool ok = true;
-    int32_t ids[RG], sid = -1, t_len = 0, t_h = 0, t_0 = 0;
+    int32_t ids[RG], sid = -1, t_len = 0, t_first = 0, t_h = 0, t_0 = 0;
     const auto look_up = [&]() {                    // false: there is no further tile
       if (tile == it.tile0 + it.tiles) {            // the next item, for everybody
         const uint32_t slot = items & (kItemRing - 1);
@@ -519,6 +519,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         if (!ok || !it.more) return false;
       }
       t_len = it.len;
+      t_first = attend_first(p, it.n, it.len);
       t_h = it.h;
       t_0 = tile++ * kTileTokens;
       const int32_t* row = p.table + (int64_t)it.r * p.width;
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
           const int32_t tok = t_0 + (lw + i * kLoadWarps) * 8 + row8, id = ids[i];
           const bool known = (uint32_t)id < (uint32_t)p.n_blocks;
           if (id != -1 && !known) bad = kErrInvalidArg;
-          off[i] = known && tok < t_len
+          off[i] = known && tok < t_len && tok >= t_first
                        ? ((((int64_t)id * p.H + t_h) << p.bt_log2) +
                           (tok & ((1 << p.bt_log2) - 1))) * D + chunk * 16
                        : -1;

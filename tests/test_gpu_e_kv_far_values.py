@@ -136,3 +136,40 @@ def test_keys_that_are_no_number_everywhere(d, n, L):
     rows = torch.zeros(got[1].shape, dtype=torch.bool, device="cuda")
     rows[n:] = True
     far.compare(got, want, rows=rows)
+
+
+@pytest.mark.parametrize("n,lens", [(1, [333, 50]), (7, [333, 50]), (160, [333, 180]), (300, [480, 310]),
+                                    (1, [9000, 50]), (90, [2100, 300])])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_values_that_no_query_sees(d, n, lens):
+    """NaN among the values that the windows of all of a request's queries have left behind, the
+    last of them just now: they change nothing."""
+    p = far.written(lens, [n, n], 2, 4, d, 16, "e4m3", "bf16", lambda v, r, pos: v)
+    codes = p["cache"].v.view(torch.uint8)
+    keep = codes.clone()
+    for window in (1, 17, 150):
+        first = lens[0] - n - window + 1
+        if first < 1:
+            continue
+        for t in {first - 1, max(first - 9, 0), max(first - 100, 0), 0}:
+            codes[p["table"][0, t // 16].long(), :, t % 16, t % d] = 0x7F
+        far.check(p, window=window)
+        codes.copy_(keep)
+
+
+@pytest.mark.parametrize("n", [1, 7, 160, 300])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_values_that_are_no_number(d, n):
+    """A NaN among the values: its column is NaN for the queries that see it; no other column, no
+    lse, no other head and no other request."""
+    L, t, col = 333, 332 - n // 2, 37
+    p = far.written([L, L], [n, n], 2, 4, d, 16, "e4m3", "bf16", lambda v, r, pos: v)
+    want = far.attend(p)
+    p["cache"].v.view(torch.uint8)[p["table"][0, t // 16].long(), 1, t % 16, col] = 0x7F
+    got = far.call(p)
+    hs.hs_get_device_error()
+    hit = far.sees(L, n, True, 0)[:, t]
+    assert torch.isnan(got[0][:n][hit][:, 4:, col].float()).all()
+    may = torch.zeros(p["q"].shape, dtype=torch.bool, device="cuda")
+    may[:n, 4:, col] = True
+    far.compare(got, want, columns=~may)
