@@ -340,9 +340,14 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
   const auto load = [&](int stage) {
     const int32_t t0 = fetch.tile * TOKENS + warp * kWarpTokens;
     int32_t left = fetch.len - t0;                        // tokens that there are
-    if ((uint32_t)id0 >= (uint32_t)p.n_blocks || (uint32_t)id1 >= (uint32_t)p.n_blocks) {
+    int32_t from = attend_first(p, fetch.n, fetch.len) - t0;  // rows before it are zeros, too
+    const bool ok0 = (uint32_t)id0 < (uint32_t)p.n_blocks, ok1 = (uint32_t)id1 < (uint32_t)p.n_blocks;
+    if (!ok0 || !ok1) {                                   // ... and those of an entry that is no block
       if (left > 0) set_error(p.err, kErrInvalidArg);
-      left = 0;
+      left = ok0 ? min(left, 16) : ok1 ? left : 0;
+      if (!ok0) from = max(from, 16);
+      id0 = ok0 ? id0 : 0;                                // (nothing is copied from there)
+      id1 = ok1 ? id1 : 0;
     }
     const uint32_t base = ring_u + stage * stage_bytes<D>();
     if (left > 0) {
@@ -353,7 +358,6 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       // rows past the end are zeros (their addresses are inside the block all the same).
       constexpr int CH = D / 16, RPI = 32 / CH;           // chunks of a row, rows of a copy
       const int r0 = lane / CH;
-      const int32_t from = attend_first(p, fetch.n, fetch.len) - t0;  // rows before it are zeros too
       const uint8_t* k0 = p.k + b0 + lane * 16;
       const uint8_t* v0 = p.v + b0 + lane * 16;
       const int64_t other = b1 - b0;                      // of the second 16 tokens
@@ -368,7 +372,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       }
       if (lane < 4) {
         const float* s = lane < 2 ? p.ks : p.vs;
-        const bool ok = (lane & 1) * 16 < left;
+        const bool ok = (lane & 1) * 16 < left && (lane & 1) * 16 + 16 > from;
         const int64_t at = (int64_t)((lane & 1) ? id1 : id0) * p.H + fetch.h;
         cp_async4_zfill(base + 2 * kWarpTokens * D + lane * 4, s + (ok ? at : 0), ok);
       }
