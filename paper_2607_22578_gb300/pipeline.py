@@ -420,11 +420,12 @@ class KvRequests:
         """The step's queries [max_tokens, n_heads, dim] over all that their
         request has.  Returns (out, lse); rows past the step's tokens are not
         written."""
-        key = (q.shape[1], cache.dim)
-        if key not in self._ws:
-            self._ws[key] = torch.zeros(
-                _lib.hs_kv_attend_workspace(cache, q.shape[1], self.max_q), dtype=torch.uint8,
-                device=q.device)
+        # One for each shape of heads, and for each stream: calls on two may run side by side.
+        key = (q.shape[1], cache.n_kv_heads, cache.dim,
+               torch.cuda.current_stream(q.device).cuda_stream)
+        size = _lib.hs_kv_attend_workspace(cache, q.shape[1], self.max_q)
+        if key not in self._ws or self._ws[key].numel() < size:
+            self._ws[key] = torch.zeros(size, dtype=torch.uint8, device=q.device)
         return _lib.hs_kv_attend(cache, q, self.lens, self.table, starts=self.starts,
                                  max_q=self.max_q, scale=scale, window=window,
                                  n_req_dev=self.n_req, workspace=self._ws[key])
