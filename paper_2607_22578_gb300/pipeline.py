@@ -390,13 +390,18 @@ class KvRequests:
         """New requests for the prompts tokens [n, stride] (int32, ``lens`` of
         them valid): equal ones are one request.  Returns (slots, starts,
         unique_idx, inverse): request u's tokens are those of prompt
-        unique_idx[u], prompt i is request inverse[i]."""
+        unique_idx[u], prompt i is request inverse[i].  The requests of an
+        earlier ``begin`` end with it: blocks that they still have go back."""
         n, stride = tokens.shape
         if n > self.max_requests:
             raise ValueError("more prompts than max_requests")
         if lens is None:
             lens = torch.full((n,), stride, dtype=torch.int32, device=tokens.device)
-        _, self.n_req, unique_idx, inverse = _lib.hs_merge_rows(tokens, lens)
+        _, n_req, unique_idx, inverse = _lib.hs_merge_rows(tokens, lens)
+        if self.starts is not None:                     # what the batch before still has
+            self.cursor = _lib.hs_kv_release(self.lens, self.table, self.pool, self.cursor,
+                                             self.block_tokens, n_req_dev=self.n_req)
+        self.n_req = n_req
         fresh = torch.zeros(self.max_requests, dtype=torch.int32, device=tokens.device)
         _lib.hs_scatter_results(lens, unique_idx, dst=fresh[:n])
         self.lens.zero_()

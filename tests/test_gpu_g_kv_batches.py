@@ -74,3 +74,22 @@ def test_each_stream_has_its_workspace():
     assert torch.equal(got[0][:n], want[0][:n])
     at = {w.data_ptr() for w in req._ws.values()}
     assert len(at) == 2
+
+
+def test_a_second_batch_gives_back_the_first_ones_blocks():
+    cache = hs.KvCache(24, BT, 2, D)
+    req = hs.KvRequests(cache, max_requests=4, max_len=200)
+    for batch, lens in enumerate(([100, 17, 40], [5], [160, 150, 30, 1], [200], [16, 16])):
+        req.begin(*prompts(lens, first=batch))
+        hs.hs_get_device_error()
+        held = sum(-(-n // BT) for n in lens)
+        taken, given = req.cursor.tolist()
+        assert given - taken == 24 - held
+        step(req, cache, 4, batch)
+        if batch == 1:                                   # some of it given back before
+            req.release(torch.tensor([True] * 4, device="cuda"))
+            assert req.cursor.tolist()[1] - req.cursor.tolist()[0] == 24
+        taken, given = req.cursor.tolist()
+        free = req.pool.cpu()[[i % 24 for i in range(taken, given)]].tolist()
+        mine = [x for r, n in enumerate(req.lens.tolist()) for x in req.table[r, :-(-n // BT)].tolist()]
+        assert sorted(free + mine) == list(range(24))
