@@ -737,9 +737,12 @@ def hs_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, slots: torch.
     shape, by = k.shape, k.stride()
     if v.shape != shape or shape[1] != cache.n_kv_heads or vtype != dtype:
         raise ValueError("k and v must both be [tokens, n_kv_heads, dim] of one dtype")
-    if v.stride() != by:
-        raise ValueError("k and v must have the same strides")
     T = shape[0]
+    other = v.stride()
+    if other != by:                             # of an axis of length 1 they say nothing
+        if (T > 1 and other[0] != by[0]) or (shape[1] > 1 and other[1] != by[1]):
+            raise ValueError("k and v must have the same strides")
+        by = (by[0] if T > 1 else 0, by[1] if shape[1] > 1 else 0)
     _check((_lib or load()).hs_kv_append(cache._at, kp, vp, dtype, T, by[0], by[1],
                                          _i32(slots, "slots", T), _stream(stream)))
 
