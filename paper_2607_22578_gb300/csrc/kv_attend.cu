@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             sum[nt][e] = 0.0f;
             const int pos = at.len - at.n + attend_query(p, at.group * ROWS + nt * 8 + 2 * c + e);
             top[nt][e] = p.causal ? min(pos, at.len - 1) : at.len - 1;
-            bottom[nt][e] = p.window > 0 ? pos - p.window + 1 : 0;
+            bottom[nt][e] = p.window > 0 ? pos - attend_window(p, at.len) + 1 : 0;
           }
         }
 #pragma unroll

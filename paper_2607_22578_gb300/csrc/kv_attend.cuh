@@ -75,10 +75,16 @@ __device__ __forceinline__ bool attend_request(const AttendParams& p, int32_t r,
   return true;
 }
 
+// A request's window: one longer than what it has hides nothing, and so 31 bits hold a position less
+// it, also of queries (2^30 at most) that stand before the first token.
+__device__ __forceinline__ int32_t attend_window(const AttendParams& p, int32_t len) {
+  return min(p.window, len);
+}
+
 // The first token that a query of a request sees.  What is before it is loaded as zeros: a weight of 0
 // would not keep a NaN among its values from the outputs.
 __device__ __forceinline__ int32_t attend_first(const AttendParams& p, int32_t n, int32_t len) {
-  return p.window > 0 ? max(len - n - p.window + 1, 0) : 0;
+  return p.window > 0 ? max(len - n - attend_window(p, len) + 1, 0) : 0;
 }
 
 static __device__ __noinline__ int32_t attend_divide(int32_t row, int32_t G) { return row / G; }

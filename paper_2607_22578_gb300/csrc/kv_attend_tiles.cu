@@ -483,7 +483,8 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             it.rows0 = max(pairs - 1 - back, 0) * kPairRows;
             const int32_t before_q = it.len - it.n;   // the first query's position
             it.tile0 = p.window > 0
-                           ? max(0, before_q + attend_query(p, it.rows0) - p.window + 1) / kTileTokens
+                           ? max(0, before_q + attend_query(p, it.rows0) - attend_window(p, it.len) +
+                                        1) / kTileTokens
                            : 0;
             const auto steps = [&](int32_t first) {   // of the tile of rows that begins there
               if (first >= it.rows) return 0;
@@ -894,12 +895,12 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             make_int4(rows0, it.rows, it.q0 * (p.H * p.G) + it.h * p.G, (int32_t)it.part);
       const int32_t pos = it.len - it.n + attend_query(p, min(rows0 + row, it.rows - 1));
       const int32_t top = p.causal ? min(pos, it.len - 1) : it.len - 1;
-      const int32_t bottom = p.window > 0 ? pos - p.window + 1 : 0;
+      const int32_t bottom = p.window > 0 ? pos - attend_window(p, it.len) + 1 : 0;
       // tokens that every row of the tile sees: from .. to
       const int32_t pos0 = it.len - it.n + attend_query(p, rows0);
       const int32_t pos1 = it.len - it.n + min(it.n - 1, attend_query(p, rows0 + kTileRows - 1));
       const int32_t to = p.causal ? min(pos0, it.len - 1) : it.len - 1;
-      const int32_t from = p.window > 0 ? pos1 - p.window + 1 : 0;
+      const int32_t from = p.window > 0 ? pos1 - attend_window(p, it.len) + 1 : 0;
       const uint32_t tile_base = tiles;
       tiles += it.tiles;
 
