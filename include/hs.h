@@ -723,6 +723,7 @@ hs_status hs_kv_append(const hs_kv_cache* cache, const void* k, const void* v, i
  *             values contiguous (16-byte aligned rows take wide loads).
  * max_q       the most queries of a request.
  * table       int32 [n_req, table_width]; the entries of L tokens are read.
+ *             table_width * block_tokens <= 2^31 - 512.
  * out         [n_tokens, n_heads, dim] of dtype, contiguous.
  * lse         float [n_tokens, n_heads], or NULL.
  * workspace   hs_kv_attend_workspace() bytes, 256-byte aligned, zeroed once

@@ -622,8 +622,9 @@ hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, i
     return fail(HS_ERR_INVALID_ARG, "n_tokens * n_heads or max_q * n_heads out of range");
   if (!starts && (int64_t)max_q * n_req > n_tokens)
     return fail(HS_ERR_INVALID_ARG, "no starts, and n_req * max_q > n_tokens");
-  if (table_width < 1 || (int64_t)table_width * cache->block_tokens > 0x7fffff00LL)
-    return fail(HS_ERR_INVALID_ARG, "table_width < 1 or table_width * block_tokens > 2^31 - 256");
+  // (a step of 384 tokens past the last has to fit in 31 bits)
+  if (table_width < 1 || (int64_t)table_width * cache->block_tokens > 0x7ffffe00LL)
+    return fail(HS_ERR_INVALID_ARG, "table_width < 1 or table_width * block_tokens > 2^31 - 512");
   if (window < 0) return fail(HS_ERR_INVALID_ARG, "window < 0");
   if (window > 0 && !causal) return fail(HS_ERR_INVALID_ARG, "a window needs causal");
   if (!(scale > 0.0f) || scale > 3.0e38f) return fail(HS_ERR_INVALID_ARG, "scale must be positive");
