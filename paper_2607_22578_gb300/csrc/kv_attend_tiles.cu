@@ -81,6 +81,7 @@ struct Item {
   int32_t tile0, tiles, rows;        // tiles of tokens; rows of the request
   int32_t steps0, steps1;            // of these for each tile of rows (0: it has no rows)
   int32_t more;                      // 0: no further item
+  int32_t first;                     // token that a query sees
   // A part of the tokens: the first part's place among the partial results (16 bits), which part
   // it is (4), how many there are for each tile of rows (4, 4).
   uint32_t part;
@@ -482,6 +483,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
             it.h = x - back * p.H;
             it.rows0 = max(pairs - 1 - back, 0) * kPairRows;
             const int32_t before_q = it.len - it.n;   // the first query's position
+            it.first = attend_first(p, it.n, it.len);
             it.tile0 = p.window > 0
                            ? max(0, before_q + attend_query(p, it.rows0) - attend_window(p, it.len) +
                                         1) / kTileTokens
@@ -520,7 +522,7 @@ __global__ void __launch_bounds__(kTilesThreads, 1) kv_attend_tiles_kernel(const
         if (!ok || !it.more) return false;
       }
       t_len = it.len;
-      t_first = attend_first(p, it.n, it.len);
+      t_first = it.first;
       t_h = it.h;
       t_0 = tile++ * kTileTokens;
       const int32_t* row = p.table + (int64_t)it.r * p.width;
