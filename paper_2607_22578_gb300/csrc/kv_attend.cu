@@ -51,6 +51,7 @@ constexpr int kSpareBytes = 25000000;
 constexpr float kLag = 8.0f;                             // of the running maximum, in powers of two
 constexpr float kShift = 7.0f;
 constexpr float kLeastScale = 1.17549435e-38f;           // 2^-126
+constexpr float kNone = -3.0e38f;                        // a maximum of nothing, and yet a number
 constexpr float kMostFactor = 8.5070592e37f;             // 2^126
 
 // Warps of a CTA, and CTAs of an SM.  Small CTAs side by side go on loading while one of them ends
@@ -490,7 +491,8 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             qs[nt][e] = __shfl_sync(0xffffffffu, back, (2 * c + e) * 4);
-            mx[nt][e] = mo[nt][e] = -INFINITY;
+            mx[nt][e] = -INFINITY;
+            mo[nt][e] = kNone;
             sum[nt][e] = 0.0f;
             const int pos = at.len - at.n + attend_query(p, at.group * ROWS + nt * 8 + 2 * c + e);
             top[nt][e] = p.causal ? min(pos, at.len - 1) : at.len - 1;
@@ -551,16 +553,25 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             }
           }
         }
-        // Scales that are no number: see below
-        int odd = 0;
-        if (!((scales[0] * 0.0f + scales[1] * 0.0f) + (scales[2] * 0.0f + scales[3] * 0.0f) == 0.0f)) {
+        // Scales that are no number: a key's makes NaN of the scores, a value's of the outputs, of the
+        // rows that see one of its tokens.  (Scales are >= 0.)
+        if (!((scales[0] + scales[1]) + (scales[2] + scales[3]) < INFINITY)) {
+          const float nan = __int_as_float(0x7fffffff);
 #pragma unroll
           for (int mt = 0; mt < 2; ++mt) {
-            if (!(scales[mt] < INFINITY)) scales[mt] = __int_as_float(0x7fffffff);
-            if (!(scales[2 + mt] < INFINITY)) {
-              scales[2 + mt] = 0.0f;
-              odd |= 1 << mt;
-            }
+            if (!(scales[mt] < INFINITY)) scales[mt] = nan;
+            if (scales[2 + mt] < INFINITY) continue;
+            scales[2 + mt] = 0.0f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                if (max(t0 + mt * 16, bottom[nt][e]) > min(t0 + mt * 16 + 15, top[nt][e])) continue;
+#pragma unroll
+                for (int hf = 0; hf < HALVES; ++hf)
+#pragma unroll
+                  for (int k = 0; k < KS; ++k) o[hf][k][nt][e] = o[hf][k][nt][2 + e] = nan;
+              }
           }
         }
         // ---- masks, running maxima
@@ -611,7 +622,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
               m = fmaxf(m, mx[nt][e]);
               n = fmaxf(n, mo[nt][e]);
               sum[nt][e] *= m == -INFINITY ? 1.0f : fast_exp2(mx[nt][e] - m);
-              const float f = n == -INFINITY ? 1.0f : fast_exp2(mo[nt][e] - n);
+              const float f = fast_exp2(mo[nt][e] - n);
               mx[nt][e] = m;
               mo[nt][e] = n;
 #pragma unroll
@@ -623,27 +634,13 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
                 }
             }
         }
-        // A value scale that is no number, for the rows that see one of its tokens: a maximum that is
-        // none either makes their weights NaN.  (A key's makes their scores so.)
-        if (odd) {
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-              for (int mt = 0; mt < 2; ++mt)
-                if ((odd >> mt & 1) && max(t0 + mt * 16, bottom[nt][e]) <=
-                                           min(t0 + mt * 16 + 15, top[nt][e]))
-                  mo[nt][e] = __int_as_float(0x7fffffff);
-        }
         // ---- the weights, and o += w . v with dim as M, rows as N, tokens as K
         float root[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e)
-            root[nt][e] = mo[nt][e] == -INFINITY ? 1.0f
-                                                 : fast_exp2(0.5f * (mx[nt][e] - mo[nt][e]));
+            root[nt][e] = fast_exp2(0.5f * (mx[nt][e] - mo[nt][e]));
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
           uint32_t pb[NT][2];
@@ -654,7 +651,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
               const float m = mx[nt][e] == -INFINITY ? 0.0f : mx[nt][e] - kShift;
               // (where no token has weight, it may be out of range)
               float f = scales[2 + mt] * root[nt][e] * root[nt][e];
-              f = f > kMostFactor ? kMostFactor : f;
+              f = fminf(f, kMostFactor);
 #pragma unroll
               for (int x = 0; x < 2; ++x) {
                 float& z = s[mt][nt][2 * x + e];
@@ -726,14 +723,14 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float m = -INFINITY, n = -INFINITY;
+        float m = -INFINITY, n = kNone;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
           m = fmaxf(m, mx_s[w][nt * 8 + 2 * c + e]);
           n = fmaxf(n, mo_s[w][nt * 8 + 2 * c + e]);
         }
         sum[nt][e] *= mx[nt][e] == -INFINITY ? 0.0f : fast_exp2(mx[nt][e] - m);
-        const float f = mo[nt][e] == -INFINITY ? 0.0f : fast_exp2(mo[nt][e] - n);
+        const float f = fast_exp2(mo[nt][e] - n);
         mx[nt][e] = m;                                      // of the CTA from here on
         mo[nt][e] = n;
 #pragma unroll
@@ -801,12 +798,12 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
       if (warp == 0) write();
     } else {
       // Partial results: the part that begins at this CTA's first unit in its slot 0, one that
-      // begins later (and so runs past its last) in slot 1.  A slot is its rows' mx, their sums, their
-      // mo, and the sums of weighted values [row][dim].
+      // begins later (and so runs past its last) in slot 1.  A slot is its rows' sums of weights, as
+      // log2 of what they are with mx, their mo, and the sums of weighted values [row][dim].
       const int64_t first = u_begin + i - 1 - (done.tile - done.tile0);   // units of the whole
       const int64_t last = first + (done.tile_end - done.tile0) - 1;
       const int32_t c0 = cta_of(first), c1 = cta_of(last);
-      constexpr int PS = ROWS * (D + 3);
+      constexpr int PS = ROWS * (D + 2);
       const int32_t odd = first > begins(c0) ? 1 : 0;                  // the first part's slot
       const auto slot_of = [&](int32_t k) {                           // of part k
         return p.partial + ((int64_t)(c0 + k) * 2 + (k == 0 ? odd : 0)) * PS;
@@ -819,15 +816,14 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
           for (int e = 0; e < 2; ++e) {
             const int row = nt * 8 + 2 * c + e;
             if (g == 0) {
-              __stcg(d + row, mx[nt][e]);
-              __stcg(d + ROWS + row, sum[nt][e]);
-              __stcg(d + 2 * ROWS + row, mo[nt][e]);
+              __stcg(d + row, mx[nt][e] + log2f(sum[nt][e]));   // (-inf of none)
+              __stcg(d + ROWS + row, mo[nt][e]);
             }
 #pragma unroll
             for (int hf = 0; hf < HALVES; ++hf)
 #pragma unroll
               for (int k = 0; k < KS; k += 2)
-                __stcg(reinterpret_cast<float4*>(d + 3 * ROWS + row * D + hf * 128 +
+                __stcg(reinterpret_cast<float4*>(d + 2 * ROWS + row * D + hf * 128 +
                                                  g * (2 * KS) + 2 * k),
                        make_float4(o[hf][k][nt][e], o[hf][k][nt][2 + e], o[hf][k + 1][nt][e],
                                    o[hf][k + 1][nt][2 + e]));
@@ -848,12 +844,13 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
 #pragma unroll
         for (int i = 0; i < NF; ++i) {
           acc[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-          m[i] = mo[i] = -INFINITY;
+          m[i] = -INFINITY;
+          mo[i] = kNone;
           l[i] = 0.0f;
         }
         for (int32_t k0 = 0; k0 < parts; k0 += UN) {
           float4 v[NF][UN];
-          float pm[NF][UN], po[NF][UN], pl[NF][UN];
+          float pm[NF][UN], po[NF][UN];
 #pragma unroll
           for (int y = 0; y < UN; ++y) {
             const bool in = k0 + y < parts;
@@ -862,9 +859,8 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             for (int i = 0; i < NF; ++i) {
               const int f = min(tid + i * THREADS, ROWS * D / 4 - 1), row = f / (D / 4);
               pm[i][y] = in ? __ldcg(d + row) : -INFINITY;
-              pl[i][y] = __ldcg(d + ROWS + row);
-              po[i][y] = in ? __ldcg(d + 2 * ROWS + row) : -INFINITY;
-              v[i][y] = __ldcg(reinterpret_cast<const float4*>(d + 3 * ROWS) + f);
+              po[i][y] = in ? __ldcg(d + ROWS + row) : kNone;
+              v[i][y] = __ldcg(reinterpret_cast<const float4*>(d + 2 * ROWS) + f);
             }
           }
 #pragma unroll
@@ -875,7 +871,7 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
               now = fmaxf(now, pm[i][y]);
               now_o = fmaxf(now_o, po[i][y]);
             }
-            const float back = mo[i] == -INFINITY ? 0.0f : fast_exp2(mo[i] - now_o);
+            const float back = fast_exp2(mo[i] - now_o);
             l[i] *= m[i] == -INFINITY ? 0.0f : fast_exp2(m[i] - now);
             m[i] = now;
             mo[i] = now_o;
@@ -885,9 +881,8 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
             acc[i].w *= back;
 #pragma unroll
             for (int y = 0; y < UN; ++y) {
-              // (a part without a maximum may have a NaN for a sum, and 0 times that is one)
-              l[i] = fmaf(pm[i][y] == -INFINITY ? 0.0f : fast_exp2(pm[i][y] - now), pl[i][y], l[i]);
-              const float w = po[i][y] == -INFINITY ? 0.0f : fast_exp2(po[i][y] - now_o);
+              l[i] += pm[i][y] == -INFINITY ? 0.0f : fast_exp2(pm[i][y] - now);
+              const float w = fast_exp2(po[i][y] - now_o);
               acc[i].x = fmaf(w, v[i][y].x, acc[i].x);
               acc[i].y = fmaf(w, v[i][y].y, acc[i].y);
               acc[i].z = fmaf(w, v[i][y].z, acc[i].z);
@@ -988,7 +983,7 @@ static int32_t few_rows(const AttendParams& p) {
 static size_t few_partial_bytes(int32_t dim) {
   const int64_t rows = dim == 64 ? 32 : 16;               // of a tile, at most
   const int64_t ctas = (int64_t)num_sms() * kAttendMaxPerSm;
-  return (size_t)(ctas * 2 * rows * (dim + 3) * 4);
+  return (size_t)(ctas * 2 * rows * (dim + 2) * 4);
 }
 
 // `rows`: of a request, at most
