@@ -21,8 +21,9 @@
 //  - Products are on mma.sync m16n8k16 with tokens as M and rows as N: a decoding step has 1 to 16
 //    rows, which would fill an eighth of a tcgen05 tile's 128, and codes go straight from shared
 //    memory to registers as half2 (exact for e4m3 and int8).
-// Measured: 256 requests of 1 to 8192 tokens, 32 / 8 heads of 128, 2.1 GB in 339 to 345 us (0.92 of
-// the copy rate); 8 of 100 to 1500 in 11.6 us, which are launch and round trips; one of 32,771 in 21.2 (67 MB).
+// Measured: 256 requests of 1 to 8192 tokens, 32 / 8 heads of 128, 2.1 GB in 338 to 345 us (0.92 of
+// the copy rate); 8 of 100 to 1500 in 12.3 us, which are launch and round trips; one of 32,771 in 21.9
+// (67 MB, of them what L2 still has).
 // Arithmetic: q as half after division by a power of two of its row (exact but below 2^-24 of the
 // row's largest), products and sums in fp32.  A row keeps two running maxima (both may lag by 8): mx
 // of the scores s and mo of s + log2 vs, with vs the values' scale of a token's block.  The weights'
@@ -56,8 +57,8 @@ constexpr float kMostFactor = 8.5070592e37f;             // 2^126
 
 // Warps of a CTA, and CTAs of an SM.  Small CTAs side by side go on loading while one of them ends
 // a (request, head, group), a single large one leaves few parts of a long one to merge.  8 of 16,000
-// tokens take 16 us with large CTAs and 29 with small ones, 8 of 500 10.7 and 8.9, 32 of 4000 18.5
-// and 16.6; at 16 they are level.
+// tokens take 17.5 us with large CTAs and 21.8 with small ones, 19 of 4000 14.4 and 15.7, 8 of 500 10.4
+// and 9.9; 32 of 4000 16.0 and 16.6, of 500 10.7 and 10.3; 64 requests of 2000, 8 heads each, 59 and 52.
 template <int D, int NT>
 constexpr int few_warps() { return D == 256 ? 7 - NT : 4; }
 template <int D, int NT>
@@ -222,8 +223,8 @@ __global__ void __launch_bounds__(WARPS * 32, attend_ctas<D, NT, WARPS>())
   }
   int64_t U = all[0] + all[1] + all[2] + all[3];
   // Where no CTA need have units of two (request, head, group)s, each takes up to `piece` of one, if
-  // that is not many more than an equal share: 48 requests of 5 queries, 24 / 4 heads of 64, 36.6 ->
-  // 27.4 us; 16 of 4000 tokens, 4 / 1 heads of 128, 17.1 -> 13.5.
+  // that is not many more than an equal share: 48 requests of 5 queries, 24 / 4 heads of 64, 43.0 ->
+  // 31.4 us; 16 of 4000 tokens, 4 / 1 heads of 128, 17.6 -> 14.3.
   int32_t piece = 0;
   if (few && U > gridDim.x) {
     const auto pieces = [&](int32_t each) {               // of so many units
@@ -971,9 +972,9 @@ hs_status launch_dim(const AttendParams& p, int32_t dim, int64_t rows, cudaStrea
 
 // Rows of a request up to which this kernel takes it, where kv_attend_tiles.cu could.  There up to
 // 256 rows cost what one does, here every 16 read the codes again: 64 requests of 2000 tokens, 8
-// heads of 128, take 114 us here and 161 there with 32 rows, 209 and 161 with 64.  But there eight
+// heads of 128, take 126 us here and 164 there with 32 rows, 232 and 165 with 64.  But there eight
 // CTAs share an item at most, here as many as there are: one request of 8192 tokens, one head and
-// 512 rows takes 28 us here and 42 there, one of 2000 tokens, 8 heads and 64 rows 17 and 27.  The two
+// 512 rows takes 28 us here and 41 there, one of 2000 tokens, 8 heads and 64 rows 18 and 26.  The two
 // are level at about one (request, head, 16 rows) for two SMs.
 static int32_t few_rows(const AttendParams& p) {
   const int64_t heads = (int64_t)p.n_req * p.H;

@@ -9,7 +9,7 @@
 // weights, the tensor cores work for the other.  Scores become weights by halves of the tokens, each
 // a step of the running maximum, and each half is handed over when it is done.
 // (Two buffers of scores of 64 tokens each instead of one of 128: a product of N = 64 takes as long
-// as one of 128, 75 clocks, and the whole 4700 clocks for 128 tokens.)
+// as one of 128, 75 clocks, and the whole 4700 clocks for 128 tokens instead of 4500.)
 //
 //   warps 0-3, 4-7   a thread a row: its query into shared memory, scores to weights, the output
 //   warps 8-14       codes from the cache's blocks, decoded to half in shared memory (swizzled;
@@ -19,16 +19,16 @@
 // CTAs are persistent, one an SM.  Work is (request, pair of tiles of rows, kv head) items, longest
 // requests first and the later pairs of a request (which see more) first, taken from a queue (a
 // counter in the workspace, drawn from an item ahead): items are few and differ by much, and in a
-// fixed order six requests behind 1,000 to 12,000 tokens took 467 us.  An item's queries and first
+// fixed order the two cases below take 378 and 485 us.  An item's queries and first
 // tokens are loaded while the one before it ends.  Which CTA computes an item changes no result.
 // Where there are fewer items than half the CTAs, an item's tokens are up to eight parts, each an item
 // of its own; a warp's rows of the parts are merged by the one that is done last (128 queries over
-// 16,384 tokens, 32 / 8 heads of 128: 313 -> 64 us).
+// 16,384 tokens, 32 / 8 heads of 128: 313 -> 62 us).
 //
-// Measured: 16 prompts of 256 to 2048 tokens, 32 / 8 heads of 128, 329 us (635 TFLOP/s); six chunks of
-// up to 1024 queries behind 1,000 to 12,000 tokens, 32 / 4 heads, 453 (732).  256 rows by 128 tokens
-// take 4500 clocks, products 2200 of them: the rest is the chain of one tile (scores loaded, maximum,
-// 64 exponentials a thread, twice, then the last product and the next scores).
+// Measured: 16 prompts of 256 to 2048 tokens, 32 / 8 heads of 128, 343 us (610 TFLOP/s); six chunks of
+// up to 1024 queries behind 1,000 to 12,000 tokens, 32 / 4 heads, 468 (710).  256 rows by 128 tokens
+// take 4650 clocks, products 2200 of them: the rest is the chain of one tile (scores loaded, maxima,
+// 64 exponentials and their factors a thread, twice, then the last product and the next scores).
 //
 // Arithmetic: q as half after division by a power of two of its row; codes as half (exact); sums
 // in fp32.  With c a score's factor and vs the values' scale of its block, a row keeps two running
@@ -36,7 +36,8 @@
 // is of z = 2^(s - ms + 7), the output's weights are w = z * vs * 2^(ms - m) as half, o = sum w code,
 // and o * 2^(m - ms) / sum is the output.  With one maximum for both, a block of zeros (scale 2^-126)
 // would drop out of the sum, or overflow it; as it is, a weight is lost where it is below 2^-126 of
-// the row's largest, whatever the scales are.
+// the row's largest, whatever the scales are.  (The second maximum and the factors: prompts 329 -> 337 us,
+// cross attention 52.4 -> 54.6.)
 #include "kv_attend.cuh"
 #include "kv_cache.cuh"
 
