@@ -427,7 +427,8 @@ class KvRequests:
     def append(self, cache: "_lib.KvCache", k: torch.Tensor, v: torch.Tensor) -> None:
         """The step's keys and values [max_tokens, n_kv_heads, dim]."""
         if self.slots is None:
-            raise ValueError("no step is begun: begin or extend says where its tokens go")
+            raise ValueError("no step is begun: begin or extend says where its tokens go, until "
+                             "fork, branch or compact")
         _lib.hs_kv_append(cache, k, v, self.slots)
 
     def attend(self, cache: "_lib.KvCache", q: torch.Tensor, scale: float | None = None,
@@ -480,8 +481,11 @@ class KvRequests:
     def fork(self, src: torch.Tensor, dst: torch.Tensor, caches) -> None:
         """Row dst[i], which has no tokens, begins as request src[i] stands (int32;
         dst[i] = src[i] or -1 makes nothing), in every one of ``caches``.  Rows
-        past n_req count only once n_req includes them."""
+        past n_req count only once n_req includes them.  A step's tokens are
+        appended to every cache first: its slots are the first holder's alone, so
+        a step begun before has none after that."""
         self._forked = True
+        self.slots = None
         self.lens, self.cursor, source, target, tokens = _lib.hs_kv_fork(
             src, dst, self.lens, self.table, self.shared, self.pool, self.cursor,
             self.block_tokens)
@@ -491,7 +495,8 @@ class KvRequests:
     def branch(self, unique_idx: torch.Tensor, inverse: torch.Tensor, caches) -> torch.Tensor:
         """Every prompt of ``begin`` goes on by itself, as request rows[i], which
         is returned (int32): the first of each merged request as that request,
-        the others as new ones behind them."""
+        the others as new ones behind them.  As for ``fork``, the step is
+        appended to every cache first."""
         n = inverse.numel()
         first = unique_idx[inverse.long()] == torch.arange(n, device=inverse.device)
         behind = self.n_req + torch.cumsum(~first, 0) - 1
