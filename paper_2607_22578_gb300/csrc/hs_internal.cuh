@@ -459,4 +459,17 @@ hs_status once_per_device(std::atomic<uint64_t>& done, F&& setup) {
   if (st == HS_OK) done.fetch_or(bit, std::memory_order_release);
   return st;
 }
+
+// Up to `bytes` of dynamic shared memory for `kernel`, before any launch of it: one that was not
+// granted more has 48 KB for its static shared memory and its dynamic one together, so that even a
+// launch of no more than 48 KB may need this.
+template <class... KArgs>
+hs_status grant_smem(std::atomic<uint64_t>& done, void (*kernel)(KArgs...), size_t bytes,
+                     const char* what) {
+  return once_per_device(done, [&] {
+    return cuda_fail(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                          (int)bytes),
+                     what);
+  });
+}
 }  // namespace hs

@@ -924,16 +924,10 @@ hs_status launch_kv_fork(const int32_t* src, const int32_t* dst, int64_t n, cons
                      shared, pool, (int32_t)n_blocks, cursor, cursor_out, source, target, tokens,
                      err};
   const size_t smem = (size_t)(n_req + n) * 4;
-  if (smem > 48 * 1024) {
-    static std::atomic<uint64_t> configured{0};
-    const hs_status st = once_per_device(configured, [] {
-      return cuda_fail(cudaFuncSetAttribute(kv_fork_kernel,
-                                            cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            2 * HS_KV_MAX_REQUESTS * 4),
-                       "kv_fork shared memory");
-    });
-    if (st != HS_OK) return st;
-  }
+  static std::atomic<uint64_t> configured{0};
+  const hs_status st = grant_smem(configured, kv_fork_kernel, 2 * HS_KV_MAX_REQUESTS * 4,
+                                  "kv_fork shared memory");
+  if (st != HS_OK) return st;
   int64_t grid = ((n > n_req / 32 ? n : n_req / 32) * 32 + kForkThreads - 1) / kForkThreads;
   if (grid < 1) grid = 1;
   if (grid > num_sms()) grid = num_sms();

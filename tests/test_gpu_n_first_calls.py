@@ -1,0 +1,32 @@
+"""Calls whose shared memory is at the most that a kernel has without asking for
+more: the sizes around it, each way in a process of its own whose first call
+that is, the smallest first."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+HERE = os.path.dirname(os.path.abspath(__file__))
+
+FORK = """
+import test_gpu_l_kv_pages as pages
+rows, bt = 8192, 16
+rng = np.random.RandomState(1)
+lens = np.concatenate([rng.randint(1, 40, 4096), np.zeros(4096, int)])
+table, shared, free = ref.requests(list(lens), bt, 20000, 2)
+pool, cursor = ref.ring(free, 20000, 19990)
+for both in (12272, 12273, 12288, 12289):      # rows and pairs
+    pairs = both - rows
+    dst = np.concatenate([4096 + rng.permutation(4096), [-1]])[:pairs]
+    pages.fork(rng.randint(0, 4096, pairs), dst, lens, table, shared, pool, cursor, bt)
+"""
+
+
+@pytest.mark.parametrize("code", [FORK], ids=["fork"])
+def test_first_call_of_a_process(code):
+    begin = "import sys\nsys.path[:0] = [%r, %r]\nimport numpy as np\nimport pages_testutil as ref\n" % (
+        os.path.dirname(HERE), HERE)
+    r = subprocess.run([sys.executable, "-c", begin + code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
