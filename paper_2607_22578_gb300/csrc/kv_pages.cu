@@ -1015,19 +1015,13 @@ hs_status launch_kv_compact(const int32_t* lens, int64_t n_req, const int32_t* n
   const int64_t entries = n_req * width;
   const int32_t words = (int32_t)((n_blocks + 31) / 32);
   const size_t smem = (size_t)words * 8;
-  if (smem > 48 * 1024) {
-    static std::atomic<uint64_t> configured{0};
-    const hs_status st = once_per_device(configured, [] {
-      for (const auto f : {kv_compact_apply_kernel<false>, kv_compact_apply_kernel<true>}) {
-        const hs_status s = cuda_fail(
-            cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kCompactMost / 4),
-            "kv_compact shared memory");
-        if (s != HS_OK) return s;
-      }
-      return HS_OK;
-    });
-    if (st != HS_OK) return st;
-  }
+  static std::atomic<uint64_t> configured[2] = {};
+  hs_status st = grant_smem(configured[0], kv_compact_apply_kernel<false>, kCompactMost / 4,
+                            "kv_compact shared memory");
+  if (st == HS_OK)
+    st = grant_smem(configured[1], kv_compact_apply_kernel<true>, kCompactMost / 4,
+                    "kv_compact shared memory");
+  if (st != HS_OK) return st;
   const auto grid = [](int64_t threads) {
     const int64_t g = (threads + kPageThreads - 1) / kPageThreads;
     return dim3((unsigned)(g < 1 ? 1 : g < num_sms() ? g : num_sms()));

@@ -23,8 +23,17 @@ for both in (12272, 12273, 12288, 12289):      # rows and pairs
     pages.fork(rng.randint(0, 4096, pairs), dst, lens, table, shared, pool, cursor, bt)
 """
 
+COMPACT = """
+import test_gpu_l_kv_pages as pages
+lens = np.array([700, 0, 33, 1599])
+for n in (196096, 196097, 196608, 196609):     # blocks
+    table, shared, _ = ref.requests(list(lens), 16, n, n, 2)
+    pages.compact(lens, table, shared, 16, in_place=%s)
+"""
 
-@pytest.mark.parametrize("code", [FORK], ids=["fork"])
+
+@pytest.mark.parametrize("code", [FORK, COMPACT % False, COMPACT % True],
+                         ids=["fork", "compact", "compact_in_place"])
 def test_first_call_of_a_process(code):
     begin = "import sys\nsys.path[:0] = [%r, %r]\nimport numpy as np\nimport pages_testutil as ref\n" % (
         os.path.dirname(HERE), HERE)
