@@ -304,16 +304,10 @@ hs_status launch_kv_tables(const int32_t* have, const int32_t* fresh, int64_t n_
   const TabParams p{have, fresh, n_req, n_req_dev, bt_log2, table, width, pool, (int32_t)n_blocks,
                     cursor, cursor_out, starts_out, lens_out, slots_out, max_tokens, err};
   const size_t smem = (size_t)(n_req + 1) * 8;
-  if (smem > 48 * 1024) {
-    static std::atomic<uint64_t> configured{0};
-    const hs_status st = once_per_device(configured, [] {
-      return cuda_fail(cudaFuncSetAttribute(kv_tables_kernel,
-                                            cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            (HS_KV_MAX_REQUESTS + 1) * 8),
-                       "kv_tables shared memory");
-    });
-    if (st != HS_OK) return st;
-  }
+  static std::atomic<uint64_t> configured{0};
+  const hs_status st = grant_smem(configured, kv_tables_kernel, (HS_KV_MAX_REQUESTS + 1) * 8,
+                                  "kv_tables shared memory");
+  if (st != HS_OK) return st;
   int64_t grid = ((max_tokens > n_req ? max_tokens : n_req) + kTabPerCta - 1) / kTabPerCta;
   if (grid < 1) grid = 1;
   if (grid > num_sms()) grid = num_sms();

@@ -31,9 +31,20 @@ for n in (196096, 196097, 196608, 196609):     # blocks
     pages.compact(lens, table, shared, 16, in_place=%s)
 """
 
+TABLES = """
+import test_gpu_a_kv_tables as tables
+rng = np.random.default_rng(3)
+for R in (6111, 6112, 6143, 6144):             # requests
+    have, fresh = rng.integers(0, 50, R), rng.integers(0, 4, R)
+    table, pool, cursor = tables.state(rng, have, fresh, 16)
+    _, _, starts, lens, _ = tables.call(have, fresh, table, pool, cursor, 16, int(fresh.sum()))
+    assert (starts == np.concatenate([[0], np.cumsum(fresh)])).all() and (lens == have + fresh).all()
+    tables.hs.hs_get_device_error()
+"""
 
-@pytest.mark.parametrize("code", [FORK, COMPACT % False, COMPACT % True],
-                         ids=["fork", "compact", "compact_in_place"])
+
+@pytest.mark.parametrize("code", [FORK, COMPACT % False, COMPACT % True, TABLES],
+                         ids=["fork", "compact", "compact_in_place", "tables"])
 def test_first_call_of_a_process(code):
     begin = "import sys\nsys.path[:0] = [%r, %r]\nimport numpy as np\nimport pages_testutil as ref\n" % (
         os.path.dirname(HERE), HERE)
