@@ -7,6 +7,7 @@
 #include <atomic>
 #include <initializer_list>
 #include <mutex>
+#include <utility>
 
 #include "hs_internal.cuh"
 #include "kv_attend.cuh"
@@ -819,6 +820,30 @@ hs_status hs_rotary_frequencies(double base, int32_t rot_dim, double factor, dou
   return HS_OK;
 }
 
+// Whether any two of n_tokens * n_heads heads of `dim` values share one.  (What lies between two
+// heads is a step of m tokens and k heads, either way: so the strides' signs do not matter.)
+static bool heads_overlap(int64_t n_tokens, int64_t token_stride, int64_t n_heads,
+                          int64_t head_stride, int32_t dim) {
+  using Wide = __int128;  // (products of counts and any strides)
+  struct Axis {
+    Wide n, by;
+  } a{n_tokens, token_stride}, b{n_heads, head_stride};
+  for (Axis* x : {&a, &b}) {
+    if (x->by < 0) x->by = -x->by;
+    if (x->n > 1 && x->by < dim) return true;
+  }
+  if (a.n < 2 || b.n < 2) return false;
+  if (a.by < b.by) std::swap(a, b);
+  if (a.by >= (b.n - 1) * b.by + dim) return false;  // all of b's lie within one step of a
+  if (a.n * b.n * dim > (a.n - 1) * a.by + (b.n - 1) * b.by + dim) return true;  // no room for all
+  for (Wide m = 1; m < a.n; ++m) {  // against the two nearest numbers of steps of b
+    const Wide at = m * a.by, k = at / b.by < b.n - 1 ? at / b.by : b.n - 1;
+    if (at - k * b.by < dim || (k + 1 < b.n && (k + 1) * b.by - at < dim)) return true;
+    if (k == b.n - 1) break;  // (further on they only part)
+  }
+  return false;
+}
+
 hs_status hs_rotary(const void* x, int64_t token_stride, int64_t head_stride, void* out,
                     int64_t out_token_stride, int64_t out_head_stride, int32_t dtype,
                     int64_t n_tokens, int32_t n_heads, int32_t dim, int32_t rot_dim,
@@ -842,16 +867,15 @@ hs_status hs_rotary(const void* x, int64_t token_stride, int64_t head_stride, vo
       return fail(HS_ERR_INVALID_ARG, "neither positions nor lens and starts");
   }
   if (n_tokens == 0) return HS_OK;
+  if (x == out && ((n_tokens > 1 && token_stride != out_token_stride) ||
+                   (n_heads > 1 && head_stride != out_head_stride)))
+    return fail(HS_ERR_INVALID_ARG, "out is x, with other strides");
+  if (heads_overlap(n_tokens, out_token_stride, n_heads, out_head_stride, dim))
+    return fail(HS_ERR_INVALID_ARG, "heads of out overlap");
   if (!x || !out || !turns) return fail(HS_ERR_INVALID_ARG, "NULL x, out or turns");
   if (!aligned(x, 2) || !aligned(out, 2) || !aligned(turns, 8) || !aligned(positions, 4) ||
       !aligned(lens, 4) || !aligned(starts, 4))
     return fail(HS_ERR_INVALID_ARG, "misaligned pointer (x, out 2 B, turns 8 B, others 4 B)");
-  if (x == out && ((n_tokens > 1 && token_stride != out_token_stride) ||
-                   (n_heads > 1 && head_stride != out_head_stride)))
-    return fail(HS_ERR_INVALID_ARG, "out is x, with other strides");
-  if ((n_tokens > 1 && out_token_stride < dim && out_token_stride > -dim) ||
-      (n_heads > 1 && out_head_stride < dim && out_head_stride > -dim))
-    return fail(HS_ERR_INVALID_ARG, "heads of out overlap: a stride is below dim");
   RotaryParams p{};
   p.x = static_cast<const uint16_t*>(x);
   p.x_token = token_stride;

@@ -1,0 +1,52 @@
+"""Outputs that lie in one another, and what the C entry points say of them
+before they touch a device (no GPU needed)."""
+import itertools
+
+import pytest
+
+from paper_2607_22578_gb300 import _lib
+
+A = 1 << 20                                            # an aligned address that nothing reads
+
+
+def status(fn, *args):
+    return getattr(_lib.load(), fn)(*args)
+
+
+def message():
+    return _lib.load().hs_last_error().decode()
+
+
+def refused(T, H, token, head, dim):
+    """Whether out's heads are said to overlap.  (turns is NULL, so that no call goes on.)"""
+    got = status("hs_rotary", A, token, head, 2 * A, token, head, 0, T, H, dim, 2, 0, None, 1.0, 0, A,
+                 None, None, 0, None, None)
+    assert got == _lib.HS_ERR_INVALID_ARG and ("overlap" in message() or "turns" in message())
+    return "overlap" in message()
+
+
+def overlap(T, H, token, head, dim):
+    at = sorted(t * token + h * head for t in range(T) for h in range(H))
+    return any(b - a < dim for a, b in zip(at, at[1:]))
+
+
+@pytest.mark.parametrize("T,H", [(1, 1), (1, 5), (4, 1), (2, 2), (3, 2), (2, 7), (5, 4)])
+@pytest.mark.parametrize("dim", [2, 3, 8])
+def test_heads_of_out_that_overlap(T, H, dim):
+    """Every layout with strides of some heads, the equal ones among them, against all pairs."""
+    strides = sorted(set(range(dim, 4 * dim + 2)) | {dim * k + j for k in (H, T, H + 1) for j in (-1, 0, 1)})
+    for token, head in itertools.product(strides, strides):
+        want = overlap(T, H, token, head, dim)
+        for a, b in ((token, head), (-token, head), (token, -head), (-token, -head)):
+            assert refused(T, H, a, b, dim) == want == overlap(T, H, a, b, dim)
+
+
+def test_heads_of_out_of_any_size():
+    """Counts and strides whose products pass 64 bits, and many steps that nearly meet."""
+    most, far = 2 ** 31 - 1, 2 ** 62
+    assert not refused(most, most, far, 128, 128) and not refused(most, most, 128, far, 128)
+    assert refused(most, most, far, far, 128) and refused(2, 2, far, far - 127, 128)
+    assert not refused(2, 2, far, far - 128, 128) and not refused(1, 2, 0, -far, 128)
+    for T, H, token, head in ((300, 300, 128000, 128128), (300, 300, 1000, 1003), (300, 3, 6400, 3201),
+                              (100, 90, 6400, 6465), (100, 100, 6400, 6464), (100, 101, 6400, 6464)):
+        assert refused(T, H, token, head, 64) == overlap(T, H, token, head, 64)
