@@ -778,7 +778,9 @@ hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, i
  *   source_out[i], target_out[i], tokens_out[i]  (int32 [n_fork]) from which
  *   block to which, and how many tokens; -1, -1, 0 where there is nothing to copy
  * New blocks are taken in the order of the pairs.  dst[i] = -1 or dst[i] =
- * src[i] makes nothing (a request goes on as itself).
+ * src[i] makes nothing (a request goes on as itself).  No array that is written
+ * overlaps another (nor does one of hs_kv_release_shared or hs_kv_compact, but
+ * where those say so).
  *   lens        device int32 [n_req]; a row that is made has 0 there
  *   lens_out    int32 [n_req], not lens itself: L for the rows made, else lens
  *   table       device int32 [n_req, table_width], in place

@@ -693,6 +693,18 @@ hs_status hs_kv_attend(const hs_kv_cache* cache, const void* q, int32_t dtype, i
 
 // ---- requests that share blocks --------------------------------------------------------------
 
+// No output begins where an input or another output does (NULL: there is none).
+static hs_status check_outputs(std::initializer_list<const void*> outputs,
+                               std::initializer_list<const void*> inputs) {
+  for (const void* const* o = outputs.begin(); o != outputs.end(); ++o) {
+    bool same = false;
+    for (const void* i : inputs) same |= i == *o;
+    for (const void* const* other = outputs.begin(); other != o; ++other) same |= *other == *o;
+    if (*o && same) return fail(HS_ERR_INVALID_ARG, "an output is an input or another output");
+  }
+  return HS_OK;
+}
+
 hs_status hs_kv_fork(const int32_t* src, const int32_t* dst, int64_t n_fork, const int32_t* lens,
                      int32_t* lens_out, int64_t n_req, int32_t block_tokens, int32_t* table,
                      int32_t table_width, int32_t* shared, const int32_t* pool, int64_t n_blocks,
@@ -717,6 +729,13 @@ hs_status hs_kv_fork(const int32_t* src, const int32_t* dst, int64_t n_fork, con
       !aligned(cursor_out, 8) || !aligned(source_out, 4) || !aligned(target_out, 4) ||
       !aligned(tokens_out, 4))
     return fail(HS_ERR_INVALID_ARG, "misaligned pointer (cursors 8 B, others 4 B)");
+  // (every CTA reads all pairs while others write what becomes of theirs)
+  const bool lists = n_fork > 0, rows = n_req > 0;
+  if (const hs_status st = check_outputs(
+          {cursor_out, shared, rows ? lens_out : nullptr, rows ? table : nullptr,
+           lists ? source_out : nullptr, lists ? target_out : nullptr, lists ? tokens_out : nullptr},
+          {cursor, pool, lens, src, dst}))
+    return st;
   return launch_kv_fork(src, dst, n_fork, lens, lens_out, n_req, block_log2(block_tokens), table,
                         table_width, shared, pool, n_blocks, cursor, cursor_out, source_out,
                         target_out, tokens_out, reinterpret_cast<cudaStream_t>(stream));
@@ -750,6 +769,10 @@ hs_status hs_kv_release_shared(const int32_t* lens, int64_t n_req, const int32_t
   if (!aligned(lens, 4) || !aligned(table, 4) || !aligned(shared, 4) || !aligned(shared_out, 4) ||
       !aligned(pool, 4) || !aligned(cursor, 8) || !aligned(cursor_out, 8))
     return fail(HS_ERR_INVALID_ARG, "misaligned pointer (cursors 8 B, others 4 B)");
+  if (const hs_status st = check_outputs(
+          {cursor_out, pool, shared_out},
+          {cursor, lens, n_req_dev, table, shared == shared_out ? nullptr : shared}))
+    return st;
   return launch_kv_release_shared(lens, n_req, n_req_dev, block_log2(block_tokens), table,
                                   table_width, shared, shared_out, pool, n_blocks, cursor,
                                   cursor_out, reinterpret_cast<cudaStream_t>(stream));
@@ -784,6 +807,12 @@ hs_status hs_kv_compact(const int32_t* lens, int64_t n_req, const int32_t* n_req
     return fail(HS_ERR_WORKSPACE, "workspace NULL or not 256-byte aligned");
   if (workspace_bytes < need)
     return fail(HS_ERR_WORKSPACE, "compact workspace too small: %zu < %zu", workspace_bytes, need);
+  if (const hs_status st = check_outputs(
+          {pool_out, cursor_out, source_out, target_out, moves_out, shared_out, workspace,
+           n_req > 0 ? table_out : nullptr},
+          {lens, n_req_dev, table == table_out ? nullptr : table,
+           shared == shared_out ? nullptr : shared}))
+    return st;
   return launch_kv_compact(lens, n_req, n_req_dev, block_log2(block_tokens), table, table_out,
                            table_width, shared, shared_out, n_blocks, pool_out, cursor_out,
                            source_out, target_out, moves_out, workspace,
@@ -928,16 +957,10 @@ hs_status hs_sample(const void* logits, int32_t dtype, int64_t n_rows, int64_t v
       !aligned(kept_out, 4))
     return fail(HS_ERR_INVALID_ARG, "misaligned pointer (logits 2 B, others 4 B)");
   // (a draw may be looked at twice, its token being noted in between)
-  const auto among = [](const void* out, std::initializer_list<const void*> others) {
-    for (const void* o : others)
-      if (out && out == o) return true;
-    return false;
-  };
-  if (among(tokens_out, {logits, u, row_of, n_dev, temperature, top_k, top_p, min_p, logprob_out,
-                         kept_out}) ||
-      among(logprob_out, {logits, u, row_of, n_dev, temperature, top_k, top_p, min_p, kept_out}) ||
-      among(kept_out, {logits, u, row_of, n_dev, temperature, top_k, top_p, min_p}))
-    return fail(HS_ERR_INVALID_ARG, "an output is an input or another output");
+  if (const hs_status st = check_outputs(
+          {tokens_out, logprob_out, kept_out},
+          {logits, u, row_of, n_dev, temperature, top_k, top_p, min_p}))
+    return st;
   SampleParams p{};
   p.logits = static_cast<const uint16_t*>(logits);
   p.stride = row_stride;

@@ -50,3 +50,50 @@ def test_heads_of_out_of_any_size():
     for T, H, token, head in ((300, 300, 128000, 128128), (300, 300, 1000, 1003), (300, 3, 6400, 3201),
                               (100, 90, 6400, 6465), (100, 100, 6400, 6464), (100, 101, 6400, 6464)):
         assert refused(T, H, token, head, 64) == overlap(T, H, token, head, 64)
+
+
+FORK = ["src", "dst", "lens", "lens_out", "table", "shared", "pool", "cursor", "after", "source", "target",
+        "tokens"]
+
+
+def fork(at, n=3, n_req=4):
+    return status("hs_kv_fork", at["src"], at["dst"], n, at["lens"], at["lens_out"], n_req, 16, at["table"], 8,
+                  at["shared"], at["pool"], 64, at["cursor"], at["after"], at["source"], at["target"],
+                  at["tokens"], None)
+
+
+RELEASE = ["lens", "n_dev", "table", "shared", "shared_out", "pool", "cursor", "after"]
+
+
+def release(at):
+    return status("hs_kv_release_shared", at["lens"], 4, at["n_dev"], 16, at["table"], 8, at["shared"],
+                  at["shared_out"], at["pool"], 64, at["cursor"], at["after"], None)
+
+
+COMPACT = ["lens", "n_dev", "table", "table_out", "shared", "shared_out", "pool", "after", "source", "target",
+           "moves", "ws"]
+
+
+def compact(at):
+    return status("hs_kv_compact", at["lens"], 4, at["n_dev"], 16, at["table"], at["table_out"], 8, at["shared"],
+                  at["shared_out"], 64, at["pool"], at["after"], at["source"], at["target"], at["moves"],
+                  at["ws"], 256, None)
+
+
+def pairs(names, written, allowed=()):
+    return [(a, b) for a, b in itertools.combinations(names, 2)
+            if (a in written or b in written) and (a, b) not in allowed]
+
+
+CASES = [(fork, FORK, a, b) for a, b in pairs(FORK, FORK[3:6] + FORK[8:])]
+CASES += [(release, RELEASE, a, b) for a, b in pairs(RELEASE, RELEASE[4:6] + RELEASE[7:], [("shared", "shared_out")])]
+CASES += [(compact, COMPACT, a, b) for a, b in pairs(COMPACT, COMPACT[3:4] + COMPACT[5:],
+                                                     [("table", "table_out"), ("shared", "shared_out")])]
+
+
+@pytest.mark.parametrize("call,names,a,b", CASES, ids=lambda x: x if isinstance(x, str) else None)
+def test_arrays_that_are_written_are_nothing_else(call, names, a, b):
+    at = {name: (i + 1) * A for i, name in enumerate(names)}
+    at[a] = at[b]
+    assert call(at) == _lib.HS_ERR_INVALID_ARG and ("output" in message() or "cursor_out" in message() or
+                                                    "lens_out" in message())
