@@ -480,15 +480,19 @@ class KvRequests:
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, caches) -> None:
         """Row dst[i], which has no tokens, begins as request src[i] stands (int32;
-        dst[i] = src[i] or -1 makes nothing), in every one of ``caches``.  Rows
-        past n_req count only once n_req includes them.  A step's tokens are
-        appended to every cache first: its slots are the first holder's alone, so
-        a step begun before has none after that."""
+        dst[i] = src[i] or -1 makes nothing), in every one of ``caches``.  n_req
+        grows to include the rows that are made, so that what they hold is
+        counted from then on.  A step's tokens are appended to every cache first:
+        its slots are the first holder's alone, so a step begun before has none
+        after that."""
         self._forked = True
         self.slots = None
         self.lens, self.cursor, source, target, tokens = _lib.hs_kv_fork(
             src, dst, self.lens, self.table, self.shared, self.pool, self.cursor,
             self.block_tokens)
+        if src.numel():
+            made = (dst != src) & (dst < self.max_requests)
+            self.n_req = torch.maximum(self.n_req, torch.where(made, dst + 1, 0).amax())
         for cache in caches:
             _lib.hs_kv_copy(cache, source, target, tokens=tokens)
 
@@ -502,7 +506,6 @@ class KvRequests:
         behind = self.n_req + torch.cumsum(~first, 0) - 1
         rows = torch.where(first, inverse, behind.to(torch.int32))
         self.fork(inverse, rows, caches)
-        self.n_req = torch.full_like(self.n_req, n)
         return rows
 
     def compact(self, caches) -> None:
