@@ -1023,6 +1023,9 @@ def hs_rotary(x: torch.Tensor, rotary: Rotary, positions: torch.Tensor | None = 
     are not written."""
     shape, by = x.shape, x.stride()
     dtype = _KV_DTYPES.get(x.dtype)
+    turns = rotary.turns
+    if not turns.is_cuda:
+        raise TypeError("rotary's turns must be on a CUDA device")
     if dtype is None or not x.is_cuda:
         raise TypeError("x must be a CUDA tensor of bfloat16 or float16")
     if len(shape) != 3 or by[2] != 1:
@@ -1049,7 +1052,7 @@ def hs_rotary(x: torch.Tensor, rotary: Rotary, positions: torch.Tensor | None = 
         np_ = None if n_req_dev is None else _i32(n_req_dev, "n_req_dev")
     _check((_lib or load()).hs_rotary(
         x.data_ptr(), by[0], by[1], out.data_ptr(), to[0], to[1], dtype, T, shape[1], shape[2],
-        rotary.rot_dim, rotary._layout, rotary.turns.data_ptr(), rotary.magnitude,
+        rotary.rot_dim, rotary._layout, turns.data_ptr(), rotary.magnitude,
         1 if inverse else 0, pp, lp, sp, n, np_, _stream(stream)))
     return out
 

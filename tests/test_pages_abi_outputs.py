@@ -1,8 +1,9 @@
-"""Outputs that lie in one another, and what the C entry points say of them
-before they touch a device (no GPU needed)."""
+"""Arrays that lie in one another or where no kernel may read them, refused
+before anything touches a device (no GPU needed)."""
 import itertools
 
 import pytest
+import torch
 
 from paper_2607_22578_gb300 import _lib
 
@@ -97,3 +98,10 @@ def test_arrays_that_are_written_are_nothing_else(call, names, a, b):
     at[a] = at[b]
     assert call(at) == _lib.HS_ERR_INVALID_ARG and ("output" in message() or "cursor_out" in message() or
                                                     "lens_out" in message())
+
+
+def test_rotary_of_a_host_is_not_handed_to_a_kernel():
+    x = torch.zeros((2, 1, 64), dtype=torch.bfloat16)
+    for r in (_lib.Rotary(64, device="cpu"), _lib.Rotary.of([1.0] * 32, device="cpu")):
+        with pytest.raises(TypeError, match="turns"):
+            _lib.hs_rotary(x, r, positions=torch.zeros(2, dtype=torch.int32))
