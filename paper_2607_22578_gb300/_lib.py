@@ -930,6 +930,8 @@ def hs_kv_compact(lens: torch.Tensor, table: torch.Tensor, shared: torch.Tensor,
     after that, or writes them to ``out``, whose first two may be ``table`` and
     ``shared`` themselves; source, target and moves are hs_kv_copy's lists and
     n_dev, for every layer's cache."""
+    if workspace is not None and not (workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA tensor")
     n, blocks = lens.numel(), shared.numel()
     at = table.shape
     if len(at) != 2 or at[0] != n:

@@ -105,3 +105,9 @@ def test_rotary_of_a_host_is_not_handed_to_a_kernel():
     for r in (_lib.Rotary(64, device="cpu"), _lib.Rotary.of([1.0] * 32, device="cpu")):
         with pytest.raises(TypeError, match="turns"):
             _lib.hs_rotary(x, r, positions=torch.zeros(2, dtype=torch.int32))
+
+
+def test_compact_with_a_workspace_of_the_host():
+    i = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(TypeError, match="workspace"):
+        _lib.hs_kv_compact(i, i.view(2, 2), i, 16, workspace=torch.zeros(512, dtype=torch.uint8))
