@@ -176,6 +176,13 @@ def _stream(stream) -> int:
     return int(stream)
 
 
+def _on(stream, device):
+    """What torch.cuda.stream takes for a call's ``stream``."""
+    if stream is None or isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(int(stream), device=device)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -819,9 +826,7 @@ def hs_kv_attend(cache: KvCache, q: torch.Tensor, lens: torch.Tensor, table: tor
                                 or not lse.is_cuda or not lse.is_contiguous()):
             raise ValueError("lse must be contiguous float32 [tokens, n_heads]")
     if workspace is None:                       # zeroed on the stream that uses it
-        on = stream if stream is None or isinstance(stream, torch.cuda.Stream) else \
-            torch.cuda.ExternalStream(int(stream), device=q.device)
-        with torch.cuda.stream(on):
+        with torch.cuda.stream(_on(stream, q.device)):
             workspace = torch.zeros(hs_kv_attend_workspace(cache, heads, max_q),
                                     dtype=torch.uint8, device=q.device)
     _check((_lib or load()).hs_kv_attend(
@@ -958,8 +963,12 @@ def hs_kv_compact(lens: torch.Tensor, table: torch.Tensor, shared: torch.Tensor,
                 _i32(source, "source", room), _i32(target, "target", room),
                 _i32(moves, "moves", 1))
     if workspace is None:
-        workspace = torch.empty(hs_kv_compact_workspace(blocks), dtype=torch.uint8,
-                                device=table.device)
+        size, dev = hs_kv_compact_workspace(blocks), table.device
+        if stream is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=dev)
+        else:                                   # of the stream that uses it: it is freed on return
+            with torch.cuda.stream(_on(stream, dev)):
+                workspace = torch.empty(size, dtype=torch.uint8, device=dev)
     _check((_lib or load()).hs_kv_compact(
         lens.data_ptr(), n, None if n_req_dev is None else _i32(n_req_dev, "n_req_dev"),
         block_tokens, table.data_ptr(), outs[0], at[1], shared.data_ptr(), outs[1], blocks,
