@@ -15,8 +15,9 @@
 //               logits' sum a whole number of 2^-42 of the bound's weight
 // (rows of up to 2048 logits are all head).  The head is put in buckets of equal width in l, whose
 // sums say in which of them a sum of weights crosses its bound, and there few logits are left.
-// Then either all that matters lies in the head, clear of what the rest's error could move, and the
-// draw is what exact sums say, or the token is left as kPending.  order_kernel takes those rows.  A
+// Then either all that matters lies in the head, clear of what the rest's error could move and of
+// how far the two kernels' sums may lie apart, and the draw is what both would say, or the token is
+// left as kPending.  order_kernel takes those rows.  A
 // logit of 16 bits has one of 65,536 values, and equal logits have equal weights, so the order
 // needs no sorting: the numbers of logits of each value say everything.  One pass over the row
 // counts them in shared memory (a word for each magnitude, 16 bits a sign, 128 KB); top-k, top-p
@@ -886,16 +887,23 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_kernel(const SampleParam
       const uint64_t all_mass = head.scan();
       above = __reduce_add_sync(0xffffffffu, lane < kHeadWarps ? sm.scan_above[lane] : 0);
 
-      // What is kept and its mass, which the rest's error makes uncertain by `off`.
+      // What is kept and its mass, uncertain by `off`: by the rest's error, and where order_kernel
+      // might be asked instead by how far its sum may lie from this one, so that a draw is decided
+      // here only if it would be decided so there: two sums of `kept` logits, each right to 2^-41 of
+      // itself and 1 for each logit, and any two of fewer logits.
       // (what is gone counts what a vector has beside the row)
       const uint32_t all = (p.vocab + part.off + 7) / 8 * 8 - gone;
       uint32_t kept = by_k ? min((uint32_t)set.k, infinite ? n : all) : with_rest ? all : n;
-      uint64_t mass = all_mass, off = 0, entry = 0;
+      uint64_t mass = all_mass, entry = 0;
+      const auto apart = [&]() { return p.either ? (mass >> 40) + 2 * (uint64_t)kept + 2 : 0; };
+      uint64_t off = 0;
       if (with_rest && kept > n) {
         // Its error: 2^-17 of it, and 2^-20 of the 1 that each of the others counted.
         mass += mass_of(S, sm.edge);
         off = mass_of((S >> 17) + ((uint64_t)(n + gone) << (kRatioLog2 - 20)), sm.edge) + 2;
       }
+      uint64_t between = apart();
+      off += between;
       bool clear = true;
 #pragma unroll 1
       for (int step = 0; step < 4 && clear; ++step) {  // top-k, top-p, min-p, the draw
@@ -915,16 +923,16 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_kernel(const SampleParam
           const float share = step == 1 ? set.top_p : set.u;
           if (step == 1 && !(share < 1.0f)) continue;
           bool more;
-          want = part_of(mass - off, share, more);
-          want = max((uint64_t)1, want + (more || step == 3));  // (of a draw's sum, more than that)
+          want = part_of(mass - off, share, more) + (more || step == 3);  // (of a draw's sum, more
+          want = want > between ? want - between : 1;                     // than that)
           most = part_of(mass + off, share, more);
-          most = max((uint64_t)1, most + (more || step == 3));
+          most = max((uint64_t)1, most + (more || step == 3)) + between;
         }
         clear = head.find(step, want, want_n, entry, upto_it, number_of_it) && upto_it >= most;
         if (step < 3) {
           mass = upto_it;
           kept = number_of_it;
-          off = 0;
+          off = between = apart();
         }
       }
       if (tid == 0) {
@@ -1628,6 +1636,7 @@ hs_status launch_sample(SampleParams p, bool fp16, cudaStream_t stream) {
   };
   // A row that is all head leaves nothing.
   p.whole = p.vocab <= kHeadMost;
+  p.either = vecs > 1024;
   // order_kernel: as few CTAs a row as its counts allow.
   int log2 = 0;
   while ((vecs + (1 << log2) - 1) >> log2 > kMostVecs) ++log2;
@@ -1637,7 +1646,7 @@ hs_status launch_sample(SampleParams p, bool fp16, cudaStream_t stream) {
   // settings each are 14 us and not 19 from 4000 logits, 16 and 19 from 8000, but 24 and 19 from
   // 16,000, 37 and 20 from 32,000; with top-p 0.95 of flat rows 17 and 17 from 8000, 30 and 17 from
   // 16,000.  In four rounds (600 draws from 32,000) it takes 74 to 79 us, after the heads 53 to 66.
-  p.all = p.n >= 4 && vecs > 1024 && p.n <= 2 * most(log2);
+  p.all = p.n >= 4 && p.either && p.n <= 2 * most(log2);
   if (!p.all) {
     // The heads: several CTAs share an SM; more of them a row where rows are few.
     int32_t heads = 1;

@@ -22,6 +22,7 @@ struct SampleParams {
   float* logprob;
   int32_t* kept;
   bool whole;  // all of a row is its head
+  bool either; // whether head_kernel sees a row at all depends on the number of draws
   bool all;    // order_kernel takes all draws, not those that are left
   unsigned* err;
 };
