@@ -888,11 +888,11 @@ hs_status hs_rotary_frequencies(double base, int32_t rot_dim, double factor, dou
  * once.
  *   x, out       device, of dtype (HS_KV_BF16 or HS_KV_FP16), [n_tokens,
  *                n_heads, dim] with strides in elements, a head's values
- *                contiguous.  out may be x, with its strides; otherwise the two
- *                do not overlap, and neither do out's heads (x's may).  16-byte
- *                aligned heads (pointers, strides a multiple of 8) take wide
- *                loads if dim is a multiple of 8 and at most 256, or dim and
- *                rot_dim are multiples of 16.
+ *                contiguous; at most 2^30 heads.  out may be x, with its strides;
+ *                otherwise the two do not overlap, and neither do out's heads
+ *                (x's may).  16-byte aligned heads (pointers, strides a multiple
+ *                of 8) take wide loads if dim is a multiple of 8 and at most 256,
+ *                or dim and rot_dim are multiples of 16.
  *   turns        device uint64 [rot_dim / 2]
  *   positions    device int32 [n_tokens], or NULL: then token starts[r] + i of
  *                request r stands at lens[r] - n + i, n = starts[r + 1] -

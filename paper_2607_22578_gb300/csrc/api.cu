@@ -883,7 +883,8 @@ hs_status hs_rotary(const void* x, int64_t token_stride, int64_t head_stride, vo
   if (const hs_status st = check_dtype(dtype)) return st;
   if (n_tokens < 0 || n_tokens > 0x7fffffffLL)
     return fail(HS_ERR_INVALID_ARG, "n_tokens outside [0, 2^31 - 1]");
-  if (n_heads < 1) return fail(HS_ERR_INVALID_ARG, "n_heads < 1");
+  if (n_heads < 1 || n_heads > (1 << 30))  // (two more than there are, in 32 bits)
+    return fail(HS_ERR_INVALID_ARG, "n_heads outside [1, 2^30]");
   if (dim < 2 || dim > 65536) return fail(HS_ERR_INVALID_ARG, "dim outside [2, 65536]");
   if (rot_dim < 2 || rot_dim > dim || rot_dim % 2)
     return fail(HS_ERR_INVALID_ARG, "rot_dim must be even, 2 to dim");

@@ -44,13 +44,20 @@ def test_heads_of_out_that_overlap(T, H, dim):
 
 def test_heads_of_out_of_any_size():
     """Counts and strides whose products pass 64 bits, and many steps that nearly meet."""
-    most, far = 2 ** 31 - 1, 2 ** 62
-    assert not refused(most, most, far, 128, 128) and not refused(most, most, 128, far, 128)
-    assert refused(most, most, far, far, 128) and refused(2, 2, far, far - 127, 128)
+    most, heads, far = 2 ** 31 - 1, 2 ** 30, 2 ** 62
+    assert not refused(most, heads, far, 128, 128) and not refused(most, heads, 128, far, 128)
+    assert refused(most, heads, far, far, 128) and refused(2, 2, far, far - 127, 128)
     assert not refused(2, 2, far, far - 128, 128) and not refused(1, 2, 0, -far, 128)
     for T, H, token, head in ((300, 300, 128000, 128128), (300, 300, 1000, 1003), (300, 3, 6400, 3201),
                               (100, 90, 6400, 6465), (100, 100, 6400, 6464), (100, 101, 6400, 6464)):
         assert refused(T, H, token, head, 64) == overlap(T, H, token, head, 64)
+
+
+def test_more_heads_than_are_counted_in_32_bits():
+    """A thread's last heads are followed by two more numbers."""
+    for n in (2 ** 30 + 1, 2 ** 31 - 2, 2 ** 31 - 1):
+        assert status("hs_rotary", A, 0, 2, 2 * A, 0, 2, 0, 1, n, 2, 2, 0, None, 1.0, 0, A, None, None, 0, None,
+                      None) == _lib.HS_ERR_INVALID_ARG and "n_heads" in message()
 
 
 FORK = ["src", "dst", "lens", "lens_out", "table", "shared", "pool", "cursor", "after", "source", "target",
