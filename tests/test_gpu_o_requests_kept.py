@@ -128,3 +128,14 @@ def test_fork_of_nobody_makes_no_requests():
     with pytest.raises(hs.HsError):
         hs.hs_get_device_error()
     assert req.n_req.item() == 2 and (req.shared == 0).all()
+
+
+def test_a_fork_that_is_refused_changes_nothing():
+    cache, req, _, _, kv = begun([20, 37])
+    slots, _ = req.extend(torch.ones(8, **ref.INT), 8, 1)
+    for src, dst in ((ref.dev([0, 1]), ref.dev([5])), (ref.dev([0]), ref.dev([5]).long())):
+        with pytest.raises((TypeError, ValueError)):
+            req.fork(src, dst, [cache])
+    assert req.slots is slots and req.n_req.item() == 2 and (req.shared == 0).all()
+    req.append(cache, kv[:8], kv[:8])
+    hs.hs_get_device_error()
