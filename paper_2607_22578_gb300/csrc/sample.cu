@@ -923,8 +923,9 @@ __global__ void __launch_bounds__(kHeadThreads, 4) head_kernel(const SampleParam
           const float share = step == 1 ? set.top_p : set.u;
           if (step == 1 && !(share < 1.0f)) continue;
           bool more;
-          want = part_of(mass - off, share, more) + (more || step == 3);  // (of a draw's sum, more
-          want = want > between ? want - between : 1;                     // than that)
+          want = part_of(mass - off, share, more);
+          want += more || step == 3;  // (of a draw's sum, more than that)
+          want = want > between ? want - between : 1;
           most = part_of(mass + off, share, more);
           most = max((uint64_t)1, most + (more || step == 3)) + between;
         }
