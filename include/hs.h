@@ -930,7 +930,8 @@ hs_status hs_rotary(const void* x, int64_t token_stride, int64_t head_stride, vo
  * u times the sum of all that is kept.  temperature 0 takes the first in the
  * order.  NaN and minus infinity are never drawn; where the largest logit is
  * infinite, only infinite ones are.
- *   logits      device, of dtype (HS_KV_BF16 or HS_KV_FP16), [n_rows, vocab],
+ *   logits      device, of dtype (HS_KV_BF16 or HS_KV_FP16; a program that
+ *               computes penalties in fp32 rounds their result first), [n_rows, vocab],
  *               row_stride elements apart, a row's values contiguous; 16-byte
  *               aligned rows are not needed.  vocab <= HS_SAMPLE_MAX_VOCAB.
  *   row_of      device int32 [n] or NULL (then n <= n_rows)

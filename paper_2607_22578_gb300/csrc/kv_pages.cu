@@ -402,7 +402,10 @@ struct ShareParams {
 // and SM), and the blocks in order are one cluster's work, 32 a thread at a time, held in registers
 // between the count and the ring.  Latency bounds all of it: 16 of 64 requests in 8192 blocks 6.8
 // us (8.4 as one cluster), 108,000 entries in 262,144 blocks 14.6 us in three kernels (41 as one
-// cluster of eight), 290,000 in 518,048 blocks 20 (29 with a cluster of eight).
+// cluster of eight), 290,000 in 518,048 blocks 20 (29 with a cluster of eight).  Those 16 requests in
+// caches of 16,384, 32,768, 65,536, 262,144 and 524,288 blocks: 11.9, 29.4, 9.7, 10.4 and 11.1 us.  The
+// first two are one CTA's, whose lanes read counts of n_blocks / 1024 blocks each, so that 16 and 32 of
+// a warp's meet in one bank.
 constexpr int32_t kShareFew = 32768;           // blocks: 128 KB
 constexpr int64_t kShareFewEntries = 16384;
 constexpr int kShareSteps = 8;  // of 4 blocks a lane, at most
@@ -628,7 +631,9 @@ struct CompactParams {
 // q-th of those that move to the q-th free number, found by bisection.  So no CTA waits for
 // another, and each does its share of the table, the lists and the counts.  Of small tables each
 // CTA marks all entries' bits itself (MARK); of others a kernel of all SMs does.  8192 blocks, 96
-// requests of up to 102: 6.7 us, and 13.7 as one cluster with a barrier between its passes.
+// requests of up to 102: 6.7 us, and 13.7 as one cluster with a barrier between its passes.  64
+// requests in 131,072, 262,144, 524,288 and 786,432 blocks: 6.6, 9.4, 19 and 17 us; a thread's words
+// are neighbours, so that lanes' words meet in banks (16 of a warp's at 524,288 blocks, 8 at 786,432).
 constexpr int32_t kCompactMost = 786432;     // blocks: 192 KB
 constexpr int64_t kCompactEntries = 16384;   // of a table that each CTA reads
 
@@ -785,7 +790,8 @@ __global__ void __launch_bounds__(kPageThreads) kv_compact_apply_kernel(const Co
   if (bad) set_error(p.err, bad);
 }
 
-// The same for any number of blocks: one cluster, which passes over the blocks in order.
+// The same for any number of blocks: one cluster, which passes over the blocks in order, five times.
+// 64 requests in 786,433 blocks 98 us (17 in one block less, by the kernels before), in 4,000,000 367.
 __global__ void __launch_bounds__(kPageThreads) kv_compact_kernel(const CompactParams p) {
   __shared__ int32_t slots[kPageWarps], slot[3];
   pdl_wait();

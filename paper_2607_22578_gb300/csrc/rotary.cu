@@ -8,7 +8,8 @@
 // Memory bounds it: each value is read and written once.  A thread keeps the sines and cosines of
 // some pairs of one token in registers and goes over heads with them.  18,400 tokens of 40 heads of
 // 128 (94 M values, 56 us at the copy rate): 63 us interleaved, 66 in halves of whole pieces, 75 in
-// halves of 45; a pair a thread, as where heads are no whole pieces of 16 bytes, takes 205.
+// halves of 45; a pair a thread, as where heads are no whole pieces of 16 bytes, takes 130, and 203 in
+// place: its loads and stores are 2 bytes a lane, and heads with gaps leave sectors written in part.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 

@@ -956,7 +956,8 @@ constexpr int kEntries = 2 * kCells;
 struct Shared {
   float hi[129], lo[129];
   // The draw, for all of the CTA: what lies here is not held in registers from barrier to barrier,
-  // and not spilled either (a cluster's barrier sends what was spilled to the second-level cache).
+  // and so is not among what is spilled (a cluster's barrier sends that to the second-level cache:
+  // 192 bytes a thread are still stored and loaded in bf16, 144 and 136 in fp16).
   struct {
     float T, top_p, min_p, u;
     int32_t k;
@@ -1643,10 +1644,15 @@ hs_status launch_sample(SampleParams p, bool fp16, cudaStream_t stream) {
   while ((vecs + (1 << log2) - 1) >> log2 > kMostVecs) ++log2;
   // By itself where it takes the draws in two rounds at most: a round is 16 us (from 4000 logits)
   // to 25 (from 128,000), and head_kernel's 8 to 15 come on top for any draw that is left.  Few
-  // draws leave none, most of the time, and neither do small vocabularies: 64 draws with other
-  // settings each are 14 us and not 19 from 4000 logits, 16 and 19 from 8000, but 24 and 19 from
-  // 16,000, 37 and 20 from 32,000; with top-p 0.95 of flat rows 17 and 17 from 8000, 30 and 17 from
-  // 16,000.  In four rounds (600 draws from 32,000) it takes 74 to 79 us, after the heads 53 to 66.
+  // draws leave none, most of the time, and neither do small vocabularies.  After the heads and
+  // alone, us, draws with settings of their own (and all with top-p 0.95 and no top-k, which leave
+  // many): 64 draws from 4000 logits 13 and 18 (13 and 17), 8000 16 and 19 (16 and 17), 16,000 24
+  // and 19 (29 and 17), 32,000 38 and 20 (41 and 18), 128,000 44 and 26 (106 and 25); 600 draws,
+  // four rounds, from 32,000 52 and 79 (67 and 74).
+  // A number of draws cannot tell these two kinds apart, so the rule is wrong for one of them at
+  // its ends: 2 draws from 128,000 13 and 21 (34 and 20: the heads are taken), 4 of them 15 and 22
+  // (34 and 20: the order); 304, which are four rounds there, 72 and 94 (143 and 91: the heads), 600
+  // 104 and 183 (266 and 178: the heads).
   p.all = p.n >= 4 && p.either && p.n <= 2 * most(log2);
   if (!p.all) {
     // The heads: several CTAs share an SM; more of them a row where rows are few.
