@@ -26,7 +26,7 @@
  * and what those calls need beside it, where merged requests part again:
  *   hs_rotary                      rotary positions of queries and keys, and their gradient
  *   hs_sample                      a token of each row of logits from a given uniform number
- *   hs_kv_fork / hs_kv_copy        requests that go on as several, sharing their full blocks
+ *   hs_kv_fork(_n) / hs_kv_copy    requests that go on as several, sharing their full blocks
  *   hs_kv_release_shared           blocks that no request holds any more back into the ring
  *   hs_kv_compact                  the blocks in use to the low end of the cache
  *
@@ -797,6 +797,21 @@ hs_status hs_kv_fork(const int32_t* src, const int32_t* dst, int64_t n_fork, con
                      int32_t table_width, int32_t* shared, const int32_t* pool, int64_t n_blocks,
                      const int64_t* cursor, int64_t* cursor_out, int32_t* source_out,
                      int32_t* target_out, int32_t* tokens_out, hs_stream_t stream);
+
+/*
+ * hs_kv_fork_n — hs_kv_fork where the number of requests is kept on the device.
+ *
+ * Rows behind that number belong to nobody, and so would what they name.
+ *   n_req_dev   device int32: how many of the n_req rows are requests
+ *   n_req_out   device int32, not n_req_dev itself: the larger of that (cut to
+ *               [0, n_req]) and one more than the last row that is made
+ */
+hs_status hs_kv_fork_n(const int32_t* src, const int32_t* dst, int64_t n_fork, const int32_t* lens,
+                       int32_t* lens_out, int64_t n_req, const int32_t* n_req_dev,
+                       int32_t* n_req_out, int32_t block_tokens, int32_t* table,
+                       int32_t table_width, int32_t* shared, const int32_t* pool, int64_t n_blocks,
+                       const int64_t* cursor, int64_t* cursor_out, int32_t* source_out,
+                       int32_t* target_out, int32_t* tokens_out, hs_stream_t stream);
 
 /*
  * hs_kv_copy — listed blocks of a cache to other places in it.

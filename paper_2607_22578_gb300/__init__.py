@@ -6,8 +6,8 @@ from ._lib import (HS_ERR_CUDA, HS_ERR_INVALID_ARG, HS_ERR_TIMEOUT, HS_ERR_UNSUP
                    HS_ERR_WORKSPACE, HS_FNV64_OFFSET_BASIS, HS_MERGE_QUERIES_MAX, HS_OK,
                    HS_KV_BF16, HS_KV_E4M3, HS_KV_FP16, HS_KV_INT8, HS_KV_MAX_REQUESTS,
                    HS_ROTARY_HALF, HS_ROTARY_INTERLEAVED, HS_SAMPLE_MAX_VOCAB, Rotary, hs_kv_compact,
-                   hs_kv_compact_workspace, hs_kv_copy, hs_kv_fork, hs_kv_release_shared, hs_rotary,
-                   hs_rotary_frequencies, hs_sample,
+                   hs_kv_compact_workspace, hs_kv_copy, hs_kv_fork, hs_kv_fork_n, hs_kv_release_shared,
+                   hs_rotary, hs_rotary_frequencies, hs_sample,
                    HS_TOPK_MAX_K, HsError, KvCache, hs_kv_append, hs_kv_attend,
                    hs_kv_attend_workspace, hs_kv_release, hs_kv_tables, hs_debug_merge_key_mask, hs_debug_retrieve_wait,
                    hs_debug_scan_wait,
@@ -26,7 +26,8 @@ __all__ = [
     "HS_KV_E4M3", "HS_KV_INT8", "HS_KV_BF16", "HS_KV_FP16", "HS_KV_MAX_REQUESTS", "KvCache",
     "hs_kv_tables", "hs_kv_release", "hs_kv_append", "hs_kv_attend", "hs_kv_attend_workspace",
     "HS_ROTARY_HALF", "HS_ROTARY_INTERLEAVED", "HS_SAMPLE_MAX_VOCAB", "Rotary", "hs_rotary",
-    "hs_rotary_frequencies", "hs_sample", "hs_kv_fork", "hs_kv_copy", "hs_kv_release_shared",
+    "hs_rotary_frequencies", "hs_sample", "hs_kv_fork", "hs_kv_fork_n", "hs_kv_copy",
+    "hs_kv_release_shared",
     "hs_kv_compact", "hs_kv_compact_workspace",
     "HsError", "hs_fingerprint", "hs_unique_inverse", "hs_unique_inverse_noalloc",
     "hs_unique_inverse_workspace", "hs_retrieve_topk", "hs_retrieve_topk_n",

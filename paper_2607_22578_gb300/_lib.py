@@ -135,6 +135,8 @@ def load(build_if_missing: bool = True) -> ctypes.CDLL:
             lib.hs_kv_attend.restype = st
             lib.hs_kv_fork.argtypes = [P, P, i64, P, P, i64, i32, P, i32, P, P, i64, P, P, P, P, P, P]
             lib.hs_kv_fork.restype = st
+            lib.hs_kv_fork_n.argtypes = [P, P, i64, P, P, i64, P, P, i32, P, i32, P, P, i64, P, P, P, P, P, P]
+            lib.hs_kv_fork_n.restype = st
             lib.hs_kv_copy.argtypes = [P, P, P, P, i64, P, P]
             lib.hs_kv_copy.restype = st
             lib.hs_kv_release_shared.argtypes = [P, i64, P, i32, P, i32, P, P, P, i64, P, P, P]
@@ -846,6 +848,19 @@ def hs_kv_fork(src: torch.Tensor, dst: torch.Tensor, lens: torch.Tensor, table: 
     for the tokens left over.  ``table`` and ``shared`` change in place.  Returns
     (lens [n_req], cursor [2], source, target, tokens [n_fork]), or writes them
     to ``out``; the last three are hs_kv_copy's lists."""
+    return _fork(src, dst, lens, table, shared, pool, cursor, block_tokens, None, out, stream)
+
+
+def hs_kv_fork_n(src: torch.Tensor, dst: torch.Tensor, lens: torch.Tensor, n_req_dev: torch.Tensor,
+                 table: torch.Tensor, shared: torch.Tensor, pool: torch.Tensor,
+                 cursor: torch.Tensor, block_tokens: int, out: tuple | None = None, stream=None):
+    """hs_kv_fork where ``n_req_dev`` [1] says how many of the rows are requests.
+    Returns a sixth, or writes it to the sixth of ``out``: that number, or one
+    more than the last row that is made."""
+    return _fork(src, dst, lens, table, shared, pool, cursor, block_tokens, n_req_dev, out, stream)
+
+
+def _fork(src, dst, lens, table, shared, pool, cursor, block_tokens, n_req_dev, out, stream):
     n, n_req = src.numel(), lens.numel()
     at = table.shape
     if len(at) != 2 or at[0] != n_req:
@@ -866,15 +881,23 @@ def hs_kv_fork(src: torch.Tensor, dst: torch.Tensor, lens: torch.Tensor, table: 
         after, moved, source, target, tokens = new(lens), new(cursor), new(src), new(src), new(src)
         outs = (after.data_ptr(), moved.data_ptr(), source.data_ptr(), target.data_ptr(),
                 tokens.data_ptr())
+        made = None if n_req_dev is None else new(n_req_dev)
     else:
-        after, moved, source, target, tokens = out
+        made = None
+        if n_req_dev is None:
+            after, moved, source, target, tokens = out
+        else:
+            after, moved, source, target, tokens, made = out
         outs = (_i32(after, "lens out", n_req), _kv_cursor(moved, "cursor out"),
                 _i32(source, "source", n), _i32(target, "target", n), _i32(tokens, "tokens", n))
-    _check((_lib or load()).hs_kv_fork(
-        src.data_ptr(), dst.data_ptr(), n, lens.data_ptr(), outs[0], n_req, block_tokens,
+    _check((_lib or load()).hs_kv_fork_n(
+        src.data_ptr(), dst.data_ptr(), n, lens.data_ptr(), outs[0], n_req,
+        None if n_req_dev is None else _i32(n_req_dev, "n_req_dev", 1),
+        None if n_req_dev is None else _i32(made, "n_req out", 1), block_tokens,
         table.data_ptr(), at[1], shared.data_ptr(), pool.data_ptr(), blocks, cp, *outs[1:],
         _stream(stream)))
-    return after, moved, source, target, tokens
+    lists = after, moved, source, target, tokens
+    return lists if n_req_dev is None else lists + (made,)
 
 
 def hs_kv_copy(cache: KvCache, source: torch.Tensor, target: torch.Tensor,

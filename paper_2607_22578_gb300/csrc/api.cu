@@ -58,7 +58,8 @@ size_t attend_workspace(int32_t, int64_t);
 hs_status launch_kv_attend(AttendParams, int32_t, int32_t, int64_t, void*, cudaStream_t);
 hs_status launch_kv_fork(const int32_t*, const int32_t*, int64_t, const int32_t*, int32_t*, int64_t,
                          int32_t, int32_t*, int32_t, int32_t*, const int32_t*, int64_t,
-                         const int64_t*, int64_t*, int32_t*, int32_t*, int32_t*, cudaStream_t);
+                         const int64_t*, int64_t*, int32_t*, int32_t*, int32_t*, const int32_t*,
+                         int32_t*, cudaStream_t);
 hs_status launch_kv_copy(const hs_kv_cache&, const int32_t*, const int32_t*, const int32_t*, int64_t,
                          const int32_t*, cudaStream_t);
 hs_status launch_kv_release_shared(const int32_t*, int64_t, const int32_t*, int32_t, const int32_t*,
@@ -710,8 +711,21 @@ hs_status hs_kv_fork(const int32_t* src, const int32_t* dst, int64_t n_fork, con
                      int32_t table_width, int32_t* shared, const int32_t* pool, int64_t n_blocks,
                      const int64_t* cursor, int64_t* cursor_out, int32_t* source_out,
                      int32_t* target_out, int32_t* tokens_out, hs_stream_t stream) {
+  return hs_kv_fork_n(src, dst, n_fork, lens, lens_out, n_req, nullptr, nullptr, block_tokens, table,
+                      table_width, shared, pool, n_blocks, cursor, cursor_out, source_out,
+                      target_out, tokens_out, stream);
+}
+
+hs_status hs_kv_fork_n(const int32_t* src, const int32_t* dst, int64_t n_fork, const int32_t* lens,
+                       int32_t* lens_out, int64_t n_req, const int32_t* n_req_dev,
+                       int32_t* n_req_out, int32_t block_tokens, int32_t* table,
+                       int32_t table_width, int32_t* shared, const int32_t* pool, int64_t n_blocks,
+                       const int64_t* cursor, int64_t* cursor_out, int32_t* source_out,
+                       int32_t* target_out, int32_t* tokens_out, hs_stream_t stream) {
   clear_msg();
-  if (const hs_status st = check_requests(n_req, nullptr)) return st;
+  if (const hs_status st = check_requests(n_req, n_req_dev)) return st;
+  if (!n_req_dev != !n_req_out)
+    return fail(HS_ERR_INVALID_ARG, "n_req_dev without n_req_out, or the reverse");
   if (n_fork < 0) return fail(HS_ERR_INVALID_ARG, "n_fork < 0");
   if (n_fork > HS_KV_MAX_REQUESTS)
     return fail(HS_ERR_UNSUPPORTED, "n_fork > %d", HS_KV_MAX_REQUESTS);
@@ -727,18 +741,19 @@ hs_status hs_kv_fork(const int32_t* src, const int32_t* dst, int64_t n_fork, con
   if (!aligned(src, 4) || !aligned(dst, 4) || !aligned(lens, 4) || !aligned(lens_out, 4) ||
       !aligned(table, 4) || !aligned(shared, 4) || !aligned(pool, 4) || !aligned(cursor, 8) ||
       !aligned(cursor_out, 8) || !aligned(source_out, 4) || !aligned(target_out, 4) ||
-      !aligned(tokens_out, 4))
+      !aligned(tokens_out, 4) || !aligned(n_req_out, 4))
     return fail(HS_ERR_INVALID_ARG, "misaligned pointer (cursors 8 B, others 4 B)");
   // (every CTA reads all pairs while others write what becomes of theirs)
   const bool lists = n_fork > 0, rows = n_req > 0;
   if (const hs_status st = check_outputs(
-          {cursor_out, shared, rows ? lens_out : nullptr, rows ? table : nullptr,
+          {cursor_out, shared, n_req_out, rows ? lens_out : nullptr, rows ? table : nullptr,
            lists ? source_out : nullptr, lists ? target_out : nullptr, lists ? tokens_out : nullptr},
-          {cursor, pool, lens, src, dst}))
+          {cursor, pool, lens, src, dst, n_req_dev}))
     return st;
   return launch_kv_fork(src, dst, n_fork, lens, lens_out, n_req, block_log2(block_tokens), table,
                         table_width, shared, pool, n_blocks, cursor, cursor_out, source_out,
-                        target_out, tokens_out, reinterpret_cast<cudaStream_t>(stream));
+                        target_out, tokens_out, n_req_dev, n_req_out,
+                        reinterpret_cast<cudaStream_t>(stream));
 }
 
 hs_status hs_kv_copy(const hs_kv_cache* cache, const int32_t* source, const int32_t* target,

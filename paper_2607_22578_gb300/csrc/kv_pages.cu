@@ -53,6 +53,8 @@ struct ForkParams {
   int32_t* source;
   int32_t* target;
   int32_t* tokens;
+  const int32_t* n_req_dev;
+  int32_t* n_req_out;  // or NULL
   unsigned* err;
 };
 
@@ -109,6 +111,7 @@ __device__ __forceinline__ bool fork_pair(const ForkParams& p, const int32_t* fi
 
 __global__ void __launch_bounds__(kForkThreads) kv_fork_kernel(const ForkParams p) {
   extern __shared__ int32_t fork_smem[];
+  __shared__ int32_t rows;                // up to the last that is made
   int32_t* first = fork_smem;             // the first pair that names a row as its own
   int32_t* before = fork_smem + p.n_req;  // new blocks before each pair
   pdl_wait();
@@ -116,6 +119,8 @@ __global__ void __launch_bounds__(kForkThreads) kv_fork_kernel(const ForkParams 
   const int tid = threadIdx.x, lane = tid & 31;
   const int64_t taken = __ldg(p.cursor), given = __ldg(p.cursor + 1);
   unsigned bad = 0;
+  int32_t last = 0;
+  if (tid == 0) rows = 0;
   for (int32_t r = tid; r < p.n_req; r += kForkThreads) first[r] = 0x7fffffff;
   __syncthreads();
   for (int32_t i = tid; i < p.n; i += kForkThreads) {
@@ -150,6 +155,8 @@ __global__ void __launch_bounds__(kForkThreads) kv_fork_kernel(const ForkParams 
       if (own[h] != 0 || len[h] < 0 || len[h] > ((int64_t)p.width << p.bt_log2)) {
         bad = kErrInvalidArg;
         len[h] = 0;
+      } else if (makes[h]) {
+        last = max(last, d[h] + 1);
       }
       tail[h] = -1;
       if (len[h] & ((1 << p.bt_log2) - 1))
@@ -162,6 +169,10 @@ __global__ void __launch_bounds__(kForkThreads) kv_fork_kernel(const ForkParams 
       if (!needs && (len[h] & ((1 << p.bt_log2) - 1))) bad = kErrInvalidArg;
       if (i < p.n) before[i] = needs;
     }
+  }
+  if (p.n_req_out) {
+    last = __reduce_max_sync(0xffffffffu, last);
+    if (lane == 0) atomicMax(&rows, last);
   }
   __syncthreads();
   const int32_t per = (p.n + kForkThreads - 1) / kForkThreads;
@@ -234,6 +245,7 @@ __global__ void __launch_bounds__(kForkThreads) kv_fork_kernel(const ForkParams 
   if (me == 0) {
     p.cursor_out[0] = taken + avail;
     p.cursor_out[1] = given;
+    if (p.n_req_out) *p.n_req_out = max(live_requests(p.n_req, p.n_req_dev), rows);
   }
   if (bad) set_error(p.err, bad);
 }
@@ -923,12 +935,13 @@ hs_status launch_kv_fork(const int32_t* src, const int32_t* dst, int64_t n, cons
                          int32_t* lens_out, int64_t n_req, int32_t bt_log2, int32_t* table,
                          int32_t width, int32_t* shared, const int32_t* pool, int64_t n_blocks,
                          const int64_t* cursor, int64_t* cursor_out, int32_t* source,
-                         int32_t* target, int32_t* tokens, cudaStream_t stream) {
+                         int32_t* target, int32_t* tokens, const int32_t* n_req_dev,
+                         int32_t* n_req_out, cudaStream_t stream) {
   unsigned* err = device_error_word();
   if (!err) return fail(HS_ERR_CUDA, "could not resolve the device error word");
   const ForkParams p{src, dst, (int32_t)n, lens, lens_out, (int32_t)n_req, bt_log2, table, width,
                      shared, pool, (int32_t)n_blocks, cursor, cursor_out, source, target, tokens,
-                     err};
+                     n_req_dev, n_req_out, err};
   const size_t smem = (size_t)(n_req + n) * 4;
   static std::atomic<uint64_t> configured{0};
   const hs_status st = grant_smem(configured, kv_fork_kernel, 2 * HS_KV_MAX_REQUESTS * 4,

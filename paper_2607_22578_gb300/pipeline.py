@@ -485,13 +485,10 @@ class KvRequests:
         counted from then on.  A step's tokens are appended to every cache first:
         its slots are the first holder's alone, so a step begun before has none
         after that."""
-        self.lens, self.cursor, source, target, tokens = _lib.hs_kv_fork(
-            src, dst, self.lens, self.table, self.shared, self.pool, self.cursor,
+        self.lens, self.cursor, source, target, tokens, self.n_req = _lib.hs_kv_fork_n(
+            src, dst, self.lens, self.n_req, self.table, self.shared, self.pool, self.cursor,
             self.block_tokens)
         self._forked, self.slots = True, None
-        if src.numel():
-            made = (dst != src) & (dst < self.max_requests)
-            self.n_req = torch.maximum(self.n_req, torch.where(made, dst + 1, 0).amax())
         for cache in caches:
             _lib.hs_kv_copy(cache, source, target, tokens=tokens)
 

@@ -139,3 +139,43 @@ def test_a_fork_that_is_refused_changes_nothing():
     assert req.slots is slots and req.n_req.item() == 2 and (req.shared == 0).all()
     req.append(cache, kv[:8], kv[:8])
     hs.hs_get_device_error()
+
+
+@pytest.mark.parametrize("n_req,want", [(3, 9), (9, 9), (10, 10), (12, 12), (13, 12), (0, 9), (-5, 9)])
+def test_the_number_of_requests_after_a_fork(n_req, want):
+    """The last row that is made counts, not rows that pairs name in vain."""
+    table = torch.full((12, 3), -1, **ref.INT)
+    table[0, :2], table[1, :1], table[9, :1] = ref.dev([3, 4]), 5, 6
+    lens = ref.dev([20, 7, 0, 0, 0, 0, 0, 0, 0, 5, 0, 0])
+    shared, pool = torch.zeros(40, **ref.INT), torch.arange(40, **ref.INT)
+    cursor = ref.dev([10, 40], torch.int64)
+    src, dst = ref.dev([0, 2, 1, 0, 12, 11, 0, 1]), ref.dev([4, 8, 3, 9, 10, 11, 12, -1])
+    for out in (False, True):
+        given = None
+        if out:
+            given = tuple(torch.zeros(n, **ref.INT) if n != 2 else torch.zeros_like(cursor)
+                          for n in (12, 2, 8, 8, 8, 1))
+        got = hs.hs_kv_fork_n(src, dst, lens, ref.dev([n_req]), table.clone(), shared.clone(), pool, cursor, BT,
+                              out=given)
+        with pytest.raises(hs.HsError):                 # row 9 has tokens, rows 12 are none
+            hs.hs_get_device_error()
+        plain = hs.hs_kv_fork(src, dst, lens, table.clone(), shared.clone(), pool, cursor, BT)
+        with pytest.raises(hs.HsError):
+            hs.hs_get_device_error()
+        assert got[5].tolist() == [want] and all(torch.equal(a, b) for a, b in zip(got, plain))
+    none = torch.zeros(0, **ref.INT)
+    got = hs.hs_kv_fork_n(none, none, lens, ref.dev([n_req]), table, shared, pool, cursor, BT)
+    assert got[5].tolist() == [min(max(n_req, 0), 12)]
+    hs.hs_get_device_error()
+
+
+def test_the_last_of_many_rows():
+    lens = torch.zeros(16384, **ref.INT)
+    table = torch.full((16384, 2), -1, **ref.INT)
+    lens[0], table[0, 0] = 3, 7
+    pool, shared = torch.arange(20000, **ref.INT), torch.zeros(20000, **ref.INT)
+    order = 1 + torch.randperm(16380, generator=ref.gen(1), device="cuda").to(torch.int32)
+    got = hs.hs_kv_fork_n(torch.zeros_like(order), order, lens, ref.dev([1]), table, shared, pool,
+                          ref.dev([8, 20000], torch.int64), BT)
+    hs.hs_get_device_error()
+    assert got[5].tolist() == [16381] and (got[0] == 3).sum() == 16381

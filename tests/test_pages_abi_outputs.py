@@ -70,6 +70,26 @@ def fork(at, n=3, n_req=4):
                   at["tokens"], None)
 
 
+def fork_n(at):
+    return status("hs_kv_fork_n", at["src"], at["dst"], 3, at["lens"], at["lens_out"], 4, at["n_dev"],
+                  at["n_out"], 16, at["table"], 8, at["shared"], at["pool"], 64, at["cursor"], at["after"],
+                  at["source"], at["target"], at["tokens"], None)
+
+
+@pytest.mark.parametrize("other", FORK + ["n_dev"])
+def test_the_count_of_requests_is_nothing_else(other):
+    at = {name: (i + 1) * A for i, name in enumerate(FORK + ["n_dev"])}
+    assert fork_n({**at, "n_out": at[other]}) == _lib.HS_ERR_INVALID_ARG and "output" in message()
+
+
+@pytest.mark.parametrize("bad,what", [(dict(n_dev=None), "n_req_dev"), (dict(n_out=None), "n_req_dev"),
+                                      (dict(n_dev=A + 2), "n_req_dev"), (dict(n_out=A + 2), "misaligned"),
+                                      (dict(src=None), "src"), (dict(after=8 * A), "cursor_out")])
+def test_fork_n_refuses(bad, what):
+    at = {name: (i + 1) * A for i, name in enumerate(FORK + ["n_dev", "n_out"])}
+    assert fork_n({**at, **bad}) == _lib.HS_ERR_INVALID_ARG and what in message()
+
+
 RELEASE = ["lens", "n_dev", "table", "shared", "shared_out", "pool", "cursor", "after"]
 
 
